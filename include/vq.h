@@ -48,8 +48,12 @@ typedef enum vq_status {
                              size beyond VQ_LINEAR_STATIC_SCRATCH_BYTES (vq_linear_static) */
     VQ_ERR_LAUNCH = 5,    /* the HIP runtime refused the launch                       */
     VQ_ERR_ARCH = 6,      /* the current device is not gfx950 (or there is no device) */
-    VQ_ERR_BITS = 7       /* w_bits is neither 8 nor 4                                */
+    VQ_ERR_BITS = 7,      /* w_bits is neither 8 nor 4                                */
+    VQ_ERR_TYPE = 8       /* a vq_dtype that the entry point does not take            */
 } vq_status;
+
+/* Types of the entry points that take more than one (those without such an argument: fp16). */
+typedef enum vq_dtype { VQ_F16 = 0, VQ_BF16 = 1, VQ_F32 = 2 } vq_dtype;
 
 #define VQ_MAX_K 131072
 #define VQ_MAX_FUSED_K 8192 /* the fused quantizers keep a token in registers */
@@ -290,6 +294,108 @@ int vq_linear_static(const void* x_f16, const float* chan_mul, const void* w, in
  */
 int vq_quantize_weight(const float* w_f32, const float* chan_s, int w_bits, void* wq_out,
                        float* w_scale, int N, int K, void* hip_stream);
+
+/*
+ * Microscaled 4-bit floating point (the MX format with e2m1 elements), beside the integer
+ * quantizers above for models that run 4-bit weights AND activations; the matrix cores multiply
+ * it as it is stored.  (No passage of the paper: its 4-bit layers keep 8-bit activations.)
+ *
+ * A row of K values is K/32 blocks.  For every block:  t[k] = float(x[k]) * chan_mul[k] rounded
+ * to fp32;  E = floor(log2(max |t|)) - 2, at least -127;  code[k] = the e2m1 number (0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 and their negatives) nearest to t[k] / 2^E, halves to the even code,
+ * beyond 6: 6.  All of it is exact but the one rounding, so that codes and scales are fully
+ * determined.  A block of zeros has E = -127 and codes 0; a block that holds an infinity or a
+ * NaN has the scale NaN (byte 255) and codes 0, and reads back as NaN.
+ *   codes   uint8 [M,K/2]: byte j of a row holds k = 2j in bits 0..3 and k = 2j+1 in bits 4..7;
+ *           bit 3 of a code is its sign, bits 0..2 number the magnitudes above
+ *   scales  uint8 [M,S], S = VQ_MX4_SCALE_STRIDE(K): byte b of a row is E + 127 of block b, the
+ *           bytes behind the last block are written as 0 and not looked at by the readers
+ * K % 32 == 0, K <= VQ_MAX_K and pointers on 16 bytes, for every entry point here.
+ *
+ * vq_mx4_quantize:   x [M,K] of type dtype (VQ_F16, VQ_BF16; VQ_F32 for weights), chan_mul fp32
+ *                    [K] or NULL: Eq. 3's 1/s for activations, s for weights.
+ * vq_mx4_dequantize: x[m,k] = code * 2^E, rounded once to dtype (any of the three).
+ * vq_gemm_mx4:       y[m,n] = sum_k xval[m,k] * wval[n,k] + bias[n] over the values that the
+ *                    codes stand for: products exact, sums in fp32 (matrix-core order, which is
+ *                    the same for every call of the same sizes), the bias added in fp32, the
+ *                    result rounded to dtype (VQ_F16 or VQ_BF16, that of bias [N] and y [M,N];
+ *                    bias may be NULL).  xq, x_scale: M rows; wq, w_scale: N rows.
+ * vq_linear_mx4:     vq_mx4_quantize of x [M,K] (VQ_F16 or VQ_BF16) into the workspace, then
+ *                    vq_gemm_mx4 with y of the same type; few tokens are one kernel that leaves
+ *                    the workspace alone.  The workspace is at least
+ *                    vq_linear_mx4_workspace_bytes(M,N,K) bytes, 16-byte aligned.
+ */
+#define VQ_MX4_BLOCK 32
+#define VQ_MX4_SCALE_STRIDE(K) (((K) / 32 + 3) / 4 * 4)
+int vq_mx4_quantize(const void* x, int dtype, const float* chan_mul, uint8_t* xq, uint8_t* x_scale, int M, int K,
+                    void* hip_stream);
+int vq_mx4_dequantize(const uint8_t* xq, const uint8_t* x_scale, void* x, int dtype, int M, int K, void* hip_stream);
+int vq_gemm_mx4(const uint8_t* xq, const uint8_t* x_scale, const uint8_t* wq, const uint8_t* w_scale,
+                const void* bias, void* y, int dtype, int M, int N, int K, void* hip_stream);
+int vq_linear_mx4(const void* x, const float* chan_mul, const uint8_t* wq, const uint8_t* w_scale, const void* bias,
+                  void* y, int dtype, void* workspace, size_t workspace_bytes, int M, int N, int K, void* hip_stream);
+/* Bytes of workspace vq_linear_mx4 needs (0 if a size is invalid).  Host-only, no HIP call. */
+size_t vq_linear_mx4_workspace_bytes(int M, int N, int K);
+
+/*
+ * The two operations of a transformer block between its QKV layer and its output layer, on the
+ * layers' own row-major buffers: q, k, v are [tokens, heads, head_dim] views whose tokens and
+ * heads are any number of elements apart (the channels of a head are contiguous), so that
+ * slices of the QKV layer's output go in as they are.  Strides are in elements and multiples
+ * of 8 (inputs: 0 too, for a row that all tokens or heads share; tokens of k and v at most 2^23
+ * apart), pointers on 16 bytes (positions, cu_q, cu_k on 4), dtype VQ_F16 or VQ_BF16.
+ *
+ * vq_rotary: rotary positions.  For pair i of a head's first rot_dim channels and the token's
+ *   position p:  angle = p * inv_freq[i],  c = amplitude * cos(angle),  s = amplitude * sin(angle),
+ *       out_a = a c - b s,   out_b = b c + a s,
+ *   with (a, b) = channels (i, i + rot_dim/2), or (2i, 2i+1) if interleaved.  The angle is
+ *   reduced in 64 bits (positions far into a long context keep it), products and sums are fp32.
+ *   Channels from rot_dim on are copied.
+ *     q, q_out   [T, q_heads, head_dim]; k, k_out likewise with k_heads (k_heads = 0: none)
+ *     positions  int32 [T], any value (the negative of a position undoes it)
+ *     inv_freq   fp32 [rot_dim/2]
+ *     strides    host, eight of them: token and head of q, q_out, k, k_out
+ *   head_dim % 8 == 0, at most VQ_MAX_HEAD_DIM; rot_dim % 8 == 0, 0 < rot_dim <= head_dim.  In place
+ *   (q_out == q with the same strides) is allowed; no other overlap is.
+ *
+ * vq_rotary_frequencies: host-only, fills inv_freq [rot_dim/2] (HOST memory) and the amplitude for it.
+ *     base^(-2i/rot_dim) as it is (VQ_ROPE_PLAIN); divided by factor (VQ_ROPE_LINEAR); with
+ *     base * factor^(rot_dim/(rot_dim-2)) for the base (VQ_ROPE_BASE); or by parts (VQ_ROPE_PARTS): pairs
+ *     that turn more than 32 times over original_length positions as they are, fewer than once
+ *     divided by factor, blended linearly in the pair's number between, and the amplitude
+ *     0.1 ln(factor) + 1 (1 for the others).  base > 1, factor >= 1; original_length is looked at by VQ_ROPE_PARTS only.
+ *
+ * vq_attention: out = softmax(softmax_scale * q k^T) v over packed sequences.
+ *     q, out     [Tq, heads, head_dim]; k, v [Tk, kv_heads, head_dim]; heads % kv_heads == 0, head h
+ *                reads head h / (heads / kv_heads) of k and v
+ *     cu_q, cu_k int32 [sequences + 1], ascending: sequence b has the query rows cu_q[b] ..
+ *                cu_q[b+1] - 1 and the key rows cu_k[b] .. cu_k[b+1] - 1; the numbers may differ
+ *                (cross attention, new tokens behind earlier ones) and may be 0
+ *     causal     0, or 1: with n queries and m keys, query i of a sequence sees its keys
+ *                0 .. i + m - n.  A query that sees none gets zeros.
+ *     strides    host, eight of them: token and head of q, k, v, out
+ *   Query rows in front of the first sequence or behind the last are left as they were.  Scores, softmax and sums
+ *   are fp32; the weights exp(score - max) are rounded to dtype for the product with v (they
+ *   multiply values of that type), their sum is taken from the fp32 ones.  Not checked on the
+ *   device: k, v of a sequence finite (a value that is not reaches all of that sequence's
+ *   rows); cu_q, cu_k ascending and within Tq, Tk (violations give unspecified values in out, never a fault).
+ *   head_dim % 8 == 0, at most VQ_MAX_HEAD_DIM.  The workspace (vq_attention_workspace_bytes, which
+ *   may be 0; 16-byte aligned) holds partial results where keys are divided among workgroups;
+ *   two calls that may overlap in time need one each.
+ */
+#define VQ_MAX_HEAD_DIM 128
+int vq_rotary(const void* q, void* q_out, const void* k, void* k_out, int dtype, const int32_t* positions,
+              const float* inv_freq, float amplitude, int interleaved, int T, int q_heads, int k_heads, int head_dim,
+              int rot_dim, const int64_t* strides, void* hip_stream);
+typedef enum vq_rope { VQ_ROPE_PLAIN = 0, VQ_ROPE_LINEAR = 1, VQ_ROPE_BASE = 2, VQ_ROPE_PARTS = 3 } vq_rope;
+int vq_rotary_frequencies(float* inv_freq, float* amplitude, int rot_dim, double base, int scaling, double factor,
+                          int original_length);
+int vq_attention(const void* q, const void* k, const void* v, void* out, int dtype, const int32_t* cu_q,
+                 const int32_t* cu_k, int sequences, int Tq, int Tk, int heads, int kv_heads, int head_dim,
+                 const int64_t* strides, float softmax_scale, int causal, void* workspace, size_t workspace_bytes,
+                 void* hip_stream);
+/* Bytes of workspace vq_attention needs for these sizes (0 too if one is invalid).  Host-only, no HIP call. */
+size_t vq_attention_workspace_bytes(int sequences, int Tq, int Tk, int heads, int kv_heads, int head_dim);
 
 /* Static, host-side description of a vq_status value (no passage of the paper: the error
  * reporting of this boundary). */

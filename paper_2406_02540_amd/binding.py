@@ -23,10 +23,11 @@ EXT_PATH = os.path.join(PKG_DIR, "_vq_torch.so")  # csrc/vq_torch.cpp
 
 VQ_OK = 0
 STATUS_NAMES = {0: "VQ_OK", 1: "VQ_ERR_NULL", 2: "VQ_ERR_SHAPE", 3: "VQ_ERR_ALIGN",
-                4: "VQ_ERR_WORKSPACE", 5: "VQ_ERR_LAUNCH", 6: "VQ_ERR_ARCH", 7: "VQ_ERR_BITS"}
+                4: "VQ_ERR_WORKSPACE", 5: "VQ_ERR_LAUNCH", 6: "VQ_ERR_ARCH", 7: "VQ_ERR_BITS", 8: "VQ_ERR_TYPE"}
 
 # name -> (restype, argtypes); mirrors include/vq.h
 _P, _I, _SZ = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+_F, _D = ctypes.c_float, ctypes.c_double
 SIGNATURES = {
     "vq_quantize_per_token": (_I, [_P, _P, _P, _P, _I, _I, _P]),
     "vq_gelu_quantize": (_I, [_P, _I, _P, _P, _P, _I, _I, _P]),
@@ -48,6 +49,15 @@ SIGNATURES = {
     "vq_hadamard_linear": (_I, [_P, _P, _P, _I, _P, _P, _P, _P, _SZ, _I, _I, _I, _P]),
     "vq_linear_static": (_I, [_P, _P, _P, _I, _P, _P, _P, _I, _I, _I, _P]),
     "vq_quantize_weight": (_I, [_P, _P, _I, _P, _P, _I, _I, _P]),
+    "vq_mx4_quantize": (_I, [_P, _I, _P, _P, _P, _I, _I, _P]),
+    "vq_mx4_dequantize": (_I, [_P, _P, _P, _I, _I, _I, _P]),
+    "vq_gemm_mx4": (_I, [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _P]),
+    "vq_linear_mx4": (_I, [_P, _P, _P, _P, _P, _P, _I, _P, _SZ, _I, _I, _I, _P]),
+    "vq_linear_mx4_workspace_bytes": (_SZ, [_I, _I, _I]),
+    "vq_rotary": (_I, [_P, _P, _P, _P, _I, _P, _P, _F, _I, _I, _I, _I, _I, _I, _P, _P]),
+    "vq_rotary_frequencies": (_I, [_P, _P, _I, _D, _I, _D, _I]),
+    "vq_attention": (_I, [_P, _P, _P, _P, _I, _P, _P, _I, _I, _I, _I, _I, _I, _P, _F, _I, _P, _SZ, _P]),
+    "vq_attention_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I, _I]),
     "vq_status_string": (ctypes.c_char_p, [_I]),
 }
 
@@ -85,7 +95,9 @@ def status_string(status: int) -> str:
 _BOUND = ("vq_quantize_per_token", "vq_gelu_quantize", "vq_layernorm_quantize", "vq_residual_quantize",
           "vq_hadamard_quantize", "vq_quantize_static", "vq_channel_absmax", "vq_balance_mask", "vq_rotate_weight",
           "vq_quantize_weight", "vq_gemm_f16", "vq_gemm_w8a8", "vq_gemm_w4a8", "vq_linear_workspace_bytes", "vq_linear",
-          "vq_linear_static", "vq_layernorm_linear", "vq_gelu_linear", "vq_residual_linear", "vq_hadamard_linear")
+          "vq_linear_static", "vq_layernorm_linear", "vq_gelu_linear", "vq_residual_linear", "vq_hadamard_linear",
+          "vq_mx4_quantize", "vq_mx4_dequantize", "vq_gemm_mx4", "vq_linear_mx4", "vq_linear_mx4_workspace_bytes",
+          "vq_rotary", "vq_attention", "vq_attention_workspace_bytes")
 
 _ext = None
 
@@ -221,3 +233,65 @@ def vq_hadamard_linear(x, chan_mul, w, w_bits, w_scale, bias=None, y=None, works
 def vq_quantize_weight(w_f32, chan_s=None, w_bits=8, stream=None):
     """W fp32 [N,K] (+ s fp32 [K]) -> (wq int8 [N,K] or packed uint8 [N,K/2], w_scale fp32 [N])."""
     return (_ext or _load()).quantize_weight(w_f32, chan_s, w_bits, stream)
+
+
+def vq_mx4_quantize(x, chan_mul=None, xq=None, x_scale=None, stream=None):
+    """x fp16, bf16 or fp32 [M,K] (* chan_mul fp32 [K]) -> microscaled 4-bit codes: (xq uint8 [M,K/2], x_scale uint8
+    [M, MX4_SCALE_STRIDE(K)])."""
+    return (_ext or _load()).mx4_quantize(x, chan_mul, xq, x_scale, stream)
+
+
+def vq_mx4_dequantize(xq, x_scale, dtype=torch.float16, x=None, stream=None):
+    """The values that the codes stand for, in fp16, bf16 or fp32 (the type of x where it is given): [M,K]."""
+    return (_ext or _load()).mx4_dequantize(xq, x_scale, dtype, x, stream)
+
+
+def vq_gemm_mx4(xq, x_scale, wq, w_scale, bias=None, y=None, dtype=torch.float16, stream=None):
+    """Codes [M,K/2] x codes [N,K/2] (+ bias [N]) -> y [M,N] in fp16 or bf16 (the type of y or bias where one is given)."""
+    return (_ext or _load()).gemm_mx4(xq, x_scale, wq, w_scale, bias, y, dtype, stream)
+
+
+def vq_linear_mx4_workspace_bytes(M, N, K) -> int:
+    return int(lib().vq_linear_mx4_workspace_bytes(int(M), int(N), int(K)))
+
+
+def MX4_SCALE_STRIDE(K) -> int:
+    """Bytes of a row of scales: K/32 of them, rounded up to four (VQ_MX4_SCALE_STRIDE of include/vq.h)."""
+    return (K // 32 + 3) // 4 * 4
+
+
+def vq_linear_mx4(x, chan_mul, w, w_scale, bias=None, y=None, workspace=None, stream=None):
+    """The microscaled 4-bit layer on fp16 or bf16 activations: x [M,K] -> y [M,N] of the same type."""
+    return (_ext or _load()).linear_mx4(x, chan_mul, w, w_scale, bias, y, workspace, stream)
+
+
+def vq_rotary(q, k, positions, inv_freq, interleaved=False, amplitude=1.0, q_out=None, k_out=None, stream=None):
+    """Rotary positions on views q [T,Hq,D] and k [T,Hk,D] (or None), fp16 or bf16; positions int32 [T], inv_freq fp32
+    [rot_dim/2] -> (q_out, k_out); q_out=q, k_out=k works in place."""
+    return (_ext or _load()).rotary(q, k, positions, inv_freq, interleaved, amplitude, q_out, k_out, stream)
+
+
+ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def vq_rotary_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, original_length=0):
+    """(inv_freq fp32 [rot_dim/2] in host memory, amplitude) for vq_rotary; scaling "plain", "linear", "base" or "parts"."""
+    if scaling not in ROPE_SCALING:
+        raise ValueError(f"scaling must be one of {tuple(ROPE_SCALING)}")
+    table, amplitude = (ctypes.c_float * max(int(rot_dim) // 2, 1))(), ctypes.c_float()
+    status = lib().vq_rotary_frequencies(table, ctypes.byref(amplitude), int(rot_dim), float(base), ROPE_SCALING[scaling],
+                                         float(factor), int(original_length))
+    if status != VQ_OK:
+        raise VqError(status, "vq_rotary_frequencies")
+    return torch.tensor(list(table), dtype=torch.float32), float(amplitude.value)
+
+
+def vq_attention_workspace_bytes(sequences, Tq, Tk, heads, kv_heads, head_dim) -> int:
+    return int(lib().vq_attention_workspace_bytes(int(sequences), int(Tq), int(Tk), int(heads), int(kv_heads), int(head_dim)))
+
+
+def vq_attention(q, k, v, cu_q, cu_k, softmax_scale=None, causal=False, out=None, workspace=None, stream=None):
+    """Softmax attention over packed sequences: views q [Tq,H,D], k and v [Tk,G,D], fp16 or bf16, sequence b between rows
+    cu[b] and cu[b+1] (int32 [sequences + 1]) -> out [Tq,H,D].  softmax_scale: 1/sqrt(D) if not given; workspace is a
+    uint8 device tensor (allocated if None).  Rows outside all sequences are not written (a new out is not cleared)."""
+    return (_ext or _load()).attention(q, k, v, cu_q, cu_k, softmax_scale, causal, out, workspace, stream)

@@ -1,6 +1,7 @@
 // C-ABI front end: argument validation, device check, kernel enqueue.
 // Declarations and the contract of every entry point are in include/vq.h.
 #include <atomic>
+#include <cmath>
 
 #include "vq.h"
 #include "vq_internal.h"
@@ -212,6 +213,33 @@ int linear_through_workspace(const vq::ProducerArgs& p, const void* w, int w_bit
     if (arch != VQ_OK) return arch;
     return enqueue_layer(p, w, w_bits, w_scale, bias_f16, y_f16, xq, x_scale, M, N, K, num_cus, (hipStream_t)hip_stream);
 }
+
+// ---- microscaled 4-bit floating point, rotary positions, attention -----------------------------------------
+
+bool misaligned4(const void* p) { return ((uintptr_t)p % 4) != 0; }
+
+int validate_mx4(int M, int K) { return M < 0 || K <= 0 || K > VQ_MAX_K || K % VQ_MX4_BLOCK != 0 ? VQ_ERR_SHAPE : VQ_OK; }
+
+int validate_mx4_gemm(const void* xq, const void* x_scale, const void* wq, const void* w_scale, const void* bias, const void* y,
+                      int dtype, int M, int N, int K) {
+    if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
+    if (N < 0 || validate_mx4(M, K) != VQ_OK) return VQ_ERR_SHAPE;
+    if (M == 0 || N == 0) return VQ_OK;
+    if (!xq || !x_scale || !wq || !w_scale || !y) return VQ_ERR_NULL;
+    if (misaligned(xq) || misaligned(x_scale) || misaligned(wq) || misaligned(w_scale) || misaligned(y) || (bias && misaligned(bias)))
+        return VQ_ERR_ALIGN;
+    return VQ_OK;
+}
+
+// A view's two strides in elements: heads and rows start on 16 bytes, what is written lies apart.
+bool strides_ok(const int64_t* s, int tokens, int heads, int head_dim, bool written) {
+    for (int i = 0; i < 2; ++i) {
+        if (s[i] < 0 || s[i] % 8 != 0 || s[i] > (int64_t)1 << 40) return false;
+        if (written && s[i] < head_dim && (i == 0 ? tokens : heads) > 1) return false;
+    }
+    return true;
+}
+constexpr int64_t kMaxKeyStride = 1 << 23;   // a tile's offsets are 32-bit
 
 }  // namespace
 
@@ -442,6 +470,167 @@ int vq_quantize_weight(const float* w_f32, const float* chan_s, int w_bits, void
                                                     (hipStream_t)hip_stream));
 }
 
+int vq_mx4_quantize(const void* x, int dtype, const float* chan_mul, uint8_t* xq, uint8_t* x_scale, int M, int K,
+                    void* hip_stream) {
+    if (dtype != VQ_F16 && dtype != VQ_BF16 && dtype != VQ_F32) return VQ_ERR_TYPE;
+    const int v = validate_mx4(M, K);
+    if (v != VQ_OK) return v;
+    if (M == 0) return VQ_OK;
+    if (!x || !xq || !x_scale) return VQ_ERR_NULL;
+    if (misaligned(x) || misaligned(xq) || misaligned(x_scale) || (chan_mul && misaligned(chan_mul))) return VQ_ERR_ALIGN;
+    const int arch = check_arch();
+    if (arch != VQ_OK) return arch;
+    return launch_status(vq::launch_mx4_quantize(x, dtype, chan_mul, xq, x_scale, M, K, (hipStream_t)hip_stream));
+}
+
+int vq_mx4_dequantize(const uint8_t* xq, const uint8_t* x_scale, void* x, int dtype, int M, int K, void* hip_stream) {
+    if (dtype != VQ_F16 && dtype != VQ_BF16 && dtype != VQ_F32) return VQ_ERR_TYPE;
+    const int v = validate_mx4(M, K);
+    if (v != VQ_OK) return v;
+    if (M == 0) return VQ_OK;
+    if (!x || !xq || !x_scale) return VQ_ERR_NULL;
+    if (misaligned(x) || misaligned(xq) || misaligned(x_scale)) return VQ_ERR_ALIGN;
+    const int arch = check_arch();
+    if (arch != VQ_OK) return arch;
+    return launch_status(vq::launch_mx4_dequantize(xq, x_scale, x, dtype, M, K, (hipStream_t)hip_stream));
+}
+
+int vq_gemm_mx4(const uint8_t* xq, const uint8_t* x_scale, const uint8_t* wq, const uint8_t* w_scale, const void* bias,
+                void* y, int dtype, int M, int N, int K, void* hip_stream) {
+    const int v = validate_mx4_gemm(xq, x_scale, wq, w_scale, bias, y, dtype, M, N, K);
+    if (v != VQ_OK) return v;
+    if (M == 0 || N == 0) return VQ_OK;
+    const int arch = check_arch();
+    if (arch != VQ_OK) return arch;
+    return launch_status(vq::launch_mx4_gemm({xq, x_scale, wq, w_scale, bias, y, M, N, K}, dtype, (hipStream_t)hip_stream));
+}
+
+size_t vq_linear_mx4_workspace_bytes(int M, int N, int K) {
+    if (N < 0 || validate_mx4(M, K) != VQ_OK) return 0;
+    return round_up((size_t)M * (size_t)(K / 2), kAlign) + round_up((size_t)M * VQ_MX4_SCALE_STRIDE(K), kAlign);
+}
+
+int vq_linear_mx4(const void* x, const float* chan_mul, const uint8_t* wq, const uint8_t* w_scale, const void* bias, void* y,
+                  int dtype, void* workspace, size_t workspace_bytes, int M, int N, int K, void* hip_stream) {
+    if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
+    if (N < 0 || validate_mx4(M, K) != VQ_OK) return VQ_ERR_SHAPE;
+    if (M == 0 || N == 0) return VQ_OK;
+    if (!workspace || !x) return VQ_ERR_NULL;
+    if (misaligned(workspace) || misaligned(x) || (chan_mul && misaligned(chan_mul))) return VQ_ERR_ALIGN;
+    if (workspace_bytes < vq_linear_mx4_workspace_bytes(M, N, K)) return VQ_ERR_WORKSPACE;
+    uint8_t* const xq = (uint8_t*)workspace;
+    uint8_t* const x_scale = xq + round_up((size_t)M * (size_t)(K / 2), kAlign);
+    int v = validate_mx4_gemm(xq, x_scale, wq, w_scale, bias, y, dtype, M, N, K);
+    if (v != VQ_OK) return v;
+    const int arch = check_arch();
+    if (arch != VQ_OK) return arch;
+    v = launch_status(vq::launch_mx4_quantize(x, dtype, chan_mul, xq, x_scale, M, K, (hipStream_t)hip_stream));
+    if (v != VQ_OK) return v;
+    return launch_status(vq::launch_mx4_gemm({xq, x_scale, wq, w_scale, bias, y, M, N, K}, dtype, (hipStream_t)hip_stream));
+}
+
+int vq_rotary(const void* q, void* q_out, const void* k, void* k_out, int dtype, const int32_t* positions,
+              const float* inv_freq, float amplitude, int interleaved, int T, int q_heads, int k_heads, int head_dim,
+              int rot_dim, const int64_t* strides, void* hip_stream) {
+    if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
+    if (T < 0 || q_heads <= 0 || k_heads < 0 || q_heads > 1 << 16 || k_heads > 1 << 16 || head_dim <= 0 || head_dim % 8 != 0 ||
+        head_dim > VQ_MAX_HEAD_DIM || rot_dim <= 0 || rot_dim % 8 != 0 || rot_dim > head_dim ||
+        (interleaved != 0 && interleaved != 1) || !std::isfinite(amplitude))
+        return VQ_ERR_SHAPE;
+    if (T == 0) return VQ_OK;
+    if (!q || !q_out || (k_heads > 0 && (!k || !k_out)) || !positions || !inv_freq || !strides) return VQ_ERR_NULL;
+    for (int i = 0; i < (k_heads > 0 ? 4 : 2); ++i)
+        if (!strides_ok(strides + 2 * i, T, i < 2 ? q_heads : k_heads, head_dim, i % 2 == 1)) return VQ_ERR_SHAPE;
+    if (q == q_out && (strides[0] != strides[2] || strides[1] != strides[3])) return VQ_ERR_SHAPE;
+    if (k_heads > 0 && k == k_out && (strides[4] != strides[6] || strides[5] != strides[7])) return VQ_ERR_SHAPE;
+    if (misaligned(q) || misaligned(q_out) || misaligned(inv_freq) || misaligned4(positions) ||
+        (k_heads > 0 && (misaligned(k) || misaligned(k_out))))
+        return VQ_ERR_ALIGN;
+    const int arch = check_arch();
+    if (arch != VQ_OK) return arch;
+    vq::RotaryArgs a{};
+    a.q = q, a.q_out = q_out, a.positions = positions, a.inv_freq = inv_freq, a.amplitude = amplitude;
+    a.T = T, a.q_heads = q_heads, a.k_heads = k_heads, a.head_dim = head_dim, a.rot_dim = rot_dim;
+    a.q_token = strides[0], a.q_head = strides[1], a.qo_token = strides[2], a.qo_head = strides[3];
+    if (k_heads > 0) {
+        a.k = k, a.k_out = k_out;
+        a.k_token = strides[4], a.k_head = strides[5], a.ko_token = strides[6], a.ko_head = strides[7];
+    }
+    return launch_status(vq::launch_rotary(a, dtype, interleaved, (hipStream_t)hip_stream));
+}
+
+int vq_rotary_frequencies(float* inv_freq, float* amplitude, int rot_dim, double base, int scaling, double factor,
+                          int original_length) {
+    if (rot_dim <= 0 || rot_dim % 2 != 0 || scaling < VQ_ROPE_PLAIN || scaling > VQ_ROPE_PARTS || !std::isfinite(base) ||
+        !(base > 1.0) || !std::isfinite(factor) || !(factor >= 1.0) || (scaling == VQ_ROPE_PARTS && original_length <= 0) ||
+        (scaling == VQ_ROPE_BASE && rot_dim <= 2))
+        return VQ_ERR_SHAPE;
+    if (!inv_freq || !amplitude) return VQ_ERR_NULL;
+    if (scaling == VQ_ROPE_BASE) base *= std::pow(factor, (double)rot_dim / (rot_dim - 2));
+    // the pair that turns `n` times over the original length, as a real number
+    const double turn = 2.0 * 3.14159265358979323846;
+    auto pair_of = [&](double n) { return rot_dim * std::log(original_length / (n * turn)) / (2.0 * std::log(base)); };
+    double low = 0, high = 0;
+    if (scaling == VQ_ROPE_PARTS) {
+        low = std::fmax(std::floor(pair_of(32.0)), 0.0);
+        high = std::fmin(std::ceil(pair_of(1.0)), rot_dim - 1.0);
+        if (high <= low) high = low + 0.001;
+    }
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / rot_dim);
+        const double part = scaling == VQ_ROPE_LINEAR ? 1.0 : scaling == VQ_ROPE_PARTS ? std::fmin(std::fmax((i - low) / (high - low), 0.0), 1.0) : 0.0;
+        inv_freq[i] = (float)(f * (1.0 - part) + f / factor * part);
+    }
+    *amplitude = scaling == VQ_ROPE_PARTS ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+    return VQ_OK;
+}
+
+size_t vq_attention_workspace_bytes(int sequences, int Tq, int Tk, int heads, int kv_heads, int head_dim) {
+    if (sequences <= 0 || Tq <= 0 || Tk < 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0 || head_dim <= 0 ||
+        head_dim % 8 != 0 || head_dim > VQ_MAX_HEAD_DIM)
+        return 0;
+    const size_t parts = (size_t)vq::attention_splits(sequences, Tq, Tk, heads, kv_heads);
+    return parts == 1 ? 0 : parts * (size_t)Tq * (size_t)heads * (size_t)(head_dim + 2) * sizeof(float);
+}
+
+int vq_attention(const void* q, const void* k, const void* v, void* out, int dtype, const int32_t* cu_q, const int32_t* cu_k,
+                 int sequences, int Tq, int Tk, int heads, int kv_heads, int head_dim, const int64_t* strides,
+                 float softmax_scale, int causal, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
+    if (sequences < 0 || Tq < 0 || Tk < 0 || heads <= 0 || kv_heads <= 0 || heads > 1 << 16 || heads % kv_heads != 0 ||
+        head_dim <= 0 || head_dim % 8 != 0 || head_dim > VQ_MAX_HEAD_DIM || (causal != 0 && causal != 1) ||
+        !std::isfinite(softmax_scale) || !(softmax_scale > 0.0f))
+        return VQ_ERR_SHAPE;
+    if (sequences == 0 || Tq == 0) return VQ_OK;
+    if (!q || !out || !cu_q || !cu_k || !strides || (Tk > 0 && (!k || !v))) return VQ_ERR_NULL;
+    for (int i = 0; i < 4; ++i) {
+        const bool keys = i == 1 || i == 2;
+        if (!strides_ok(strides + 2 * i, keys ? Tk : Tq, keys ? kv_heads : heads, head_dim, i == 3)) return VQ_ERR_SHAPE;
+        if (keys && strides[2 * i] > kMaxKeyStride) return VQ_ERR_SHAPE;
+    }
+    if (misaligned(q) || misaligned(out) || (Tk > 0 && (misaligned(k) || misaligned(v))) || misaligned4(cu_q) || misaligned4(cu_k))
+        return VQ_ERR_ALIGN;
+    const size_t need = vq_attention_workspace_bytes(sequences, Tq, Tk, heads, kv_heads, head_dim);
+    if (need > 0) {
+        if (!workspace) return VQ_ERR_NULL;
+        if (misaligned(workspace)) return VQ_ERR_ALIGN;
+        if (workspace_bytes < need) return VQ_ERR_WORKSPACE;
+    }
+    const int arch = check_arch();
+    if (arch != VQ_OK) return arch;
+    vq::AttentionArgs a{};
+    a.q = q, a.k = k, a.v = v, a.out = out, a.cu_q = cu_q, a.cu_k = cu_k;
+    a.sequences = sequences, a.Tq = Tq, a.Tk = Tk, a.heads = heads, a.kv_heads = kv_heads, a.group = heads / kv_heads;
+    a.head_dim = head_dim, a.causal = causal;
+    a.q_token = strides[0], a.q_head = strides[1], a.k_token = strides[2], a.k_head = strides[3];
+    a.v_token = strides[4], a.v_head = strides[5], a.o_token = strides[6], a.o_head = strides[7];
+    a.scale_log2 = (float)((double)softmax_scale * 1.44269504088896340736);
+    a.splits = vq::attention_splits(sequences, Tq, Tk, heads, kv_heads);
+    a.part_o = (float*)workspace;
+    a.part_ml = a.part_o ? a.part_o + (size_t)a.splits * Tq * heads * head_dim : nullptr;
+    return launch_status(vq::launch_attention(a, dtype, (hipStream_t)hip_stream));
+}
+
 const char* vq_status_string(int status) {
     switch (status) {
         case VQ_OK: return "ok";
@@ -452,6 +641,7 @@ const char* vq_status_string(int status) {
         case VQ_ERR_LAUNCH: return "kernel launch failed";
         case VQ_ERR_ARCH: return "current device is not gfx950";
         case VQ_ERR_BITS: return "w_bits must be 8 or 4";
+        case VQ_ERR_TYPE: return "a type that this call does not take";
         default: return "unknown status";
     }
 }

@@ -1,0 +1,117 @@
+// Attention over packed sequences: what its kernels share.  gfx950 only.
+//
+// For the query rows of a tile and the keys in turn, with m the largest score of a row so far:
+//     S = scale * Q K^T,  m' = max(m, rowmax S),  P = exp(S - m'),  l = l exp(m - m') + rowsum P,  O = O exp(m - m') + P V
+// and O / l at the end: one pass over K and V, nothing of S leaves the registers.
+//
+// The matrix cores compute S^T = K Q^T and O^T = V^T P^T in blocks of 32 x 32 x 16: a lane's column is a query row, so that a
+// row's maximum and sum are a lane's own values and one exchange with the other half of the wavefront, and
+// the P^T that it holds after the exponentials is the operand of the second product as it lies: a lane has keys 8i + 4h + 0..3
+// (h its half), and since the order of keys in a product is free, V^T is read in that order too (transposed on its way from
+// LDS, four keys a read).
+//
+// Query heads that share a head of K and V are rows of one tile: row r of a sequence is token r / group, head r % group.
+#pragma once
+#include "vq_gemm_common.h"
+#include "vq_internal.h"
+#include "vq_types.h"
+
+namespace vq {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef short v8s __attribute__((ext_vector_type(8)));
+
+// ---- sequences -----------------------------------------------------------------------------------------------
+
+// What a workgroup works on.  The offsets come from device memory: whatever they are, rows stay within the tensors.
+struct Span {
+    int q0, n, k0, m;       // first query row and rows, first key and keys
+};
+__device__ __forceinline__ Span span_of(const AttentionArgs& a, int b) {
+    Span s;
+    s.q0 = min(max(a.cu_q[b], 0), a.Tq);
+    s.n = min(max(a.cu_q[b + 1], s.q0), a.Tq) - s.q0;
+    s.k0 = min(max(a.cu_k[b], 0), a.Tk);
+    s.m = min(max(a.cu_k[b + 1], s.k0), a.Tk) - s.k0;
+    return s;
+}
+
+// ---- tiles of K and V in LDS ---------------------------------------------------------------------------------
+// [key][CHUNKS of 16 bytes], the chunk of a key at chunk ^ swizzle(key), so that what the LDS serves at once lies in different banks:
+// K is read 16 bytes a lane, one chunk of 32 keys at a time (sixteen lanes are served together: keys 0-3, 12-15 and 20-27, or the
+// others); V transposed, 8 bytes a lane, 64 bytes of keys 4i .. 4i+3 at a time.
+template <int CHUNKS>
+__device__ __forceinline__ int k_swizzle(int key) {
+    return CHUNKS == 16 ? key & 15 : CHUNKS == 12 ? (key >> 2) & 3 : (key >> 1) & 7;
+}
+template <int CHUNKS>
+__device__ __forceinline__ int v_swizzle(int key) {
+    return CHUNKS == 16 ? (key & 3) << 2 : CHUNKS == 12 ? 0 : (key >> 1 & 1) << 2;
+}
+
+constexpr int kBehind = 0x7FFFFFF0;        // an offset that no buffer reaches: its lanes load zeros
+
+// Asks for KEYS rows of K or V, THREADS threads together.  `base` is the first of them, keys at or behind `left` and channels
+// behind the head's come as zeros.  A row's stride is at most 2^24 bytes.
+template <int CHUNKS, int KEYS, int THREADS, bool IS_V>
+__device__ __forceinline__ void load_tile(const void* base, unsigned lds, int stride, int left, int head_bytes, int thread) {
+    static_assert(KEYS * CHUNKS % THREADS == 0, "whole turns");
+    const v4i rsrc = make_rsrc(base, 0x7FFFFF00u);
+    const unsigned wave_lds = __builtin_amdgcn_readfirstlane(lds + (thread & ~63) * 16);
+#pragma unroll
+    for (int i = 0; i < KEYS * CHUNKS / THREADS; ++i) {
+        const int p = i * THREADS + thread;
+        const int key = p / CHUNKS, slot = p % CHUNKS;
+        const int c = slot ^ (IS_V ? v_swizzle<CHUNKS>(key) : k_swizzle<CHUNKS>(key));
+        const int at = key < left && 16 * c < head_bytes ? key * stride + 16 * c : kBehind;
+        load_to_lds_16(rsrc, wave_lds + i * THREADS * 16, at, 0);
+    }
+}
+
+template <class TYPE>
+__device__ __forceinline__ v16f mfma(v8s a, v8s b, v16f c);
+template <>
+__device__ __forceinline__ v16f mfma<F16>(v8s a, v8s b, v16f c) {
+    typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ v16f mfma<BF16>(v8s a, v8s b, v16f c) {
+    typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+}
+
+typedef __attribute__((address_space(3))) char* lds_bytes;
+
+// Rows `lane % 32` of the 32 keys from `key0`, channels 16 step + 8 (lane / 32) .. + 7.
+template <int CHUNKS>
+__device__ __forceinline__ v8s read_k(lds_bytes tile, int key0, int step, int lane) {
+    const int key = key0 + (lane & 31), c = (2 * step + (lane >> 5)) ^ k_swizzle<CHUNKS>(key);
+    return *(__attribute__((address_space(3))) v8s*)(tile + (key * CHUNKS + c) * 16);
+}
+
+// Channel 32 block + lane % 32 of keys key0 + 4h .. + 3 and key0 + 8 + 4h .. + 3, h = lane / 32.  In a transposed read sixteen
+// lanes name four rows of sixteen channels, four lanes a row, and each receives a column.
+template <int CHUNKS>
+__device__ __forceinline__ v8s read_v(lds_bytes tile, int key0, int block, int lane) {
+    const int in16 = lane & 15;
+    const int key = key0 + 4 * (lane >> 5) + (in16 >> 2), c = 4 * block + 2 * (lane >> 4 & 1) + (in16 >> 1 & 1);
+    lds_bytes at = tile + (key * CHUNKS + (c ^ v_swizzle<CHUNKS>(key))) * 16 + 8 * (in16 & 1);
+    // (eight keys further the swizzle is the same)
+    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)at);
+    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 8 * CHUNKS * 16));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// The key of register r of a block of S^T, less the block's first.
+__device__ __forceinline__ constexpr int key_of(int r) { return (r & 3) + 8 * (r >> 2); }   // + 4 (lane / 32)
+
+__device__ __forceinline__ float other_half(float v) {
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    // (r[0]: the low half's value in both halves, r[1]: the high half's)
+    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+}  // namespace vq

@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "vq.h"
+
 namespace vq {
 
 // A kernel of one argument.  (An argument costs the host 0.04 us, the <<<>>> stub 0.15 us beyond the 2.1 that a launch
@@ -73,6 +75,55 @@ GemmChoice choose_gemm(int w_bits, int M, int N, int K, int num_cus);
 bool small_layer(int producer, int M, int N, int K, int num_cus);
 hipError_t launch_linear_small(const ProducerArgs& p, const void* w, int w_bits, const float* w_scale, const void* bias_f16,
                                void* y_f16, int M, int N, int K, hipStream_t stream);
+
+// ---- microscaled 4-bit floating point (vq_mx4_quantize.hip, vq_mx4_gemm_split.hip) -----------------------------
+hipError_t launch_mx4_quantize(const void* x, int dtype, const float* chan_mul, uint8_t* xq, uint8_t* x_scale, int M, int K,
+                               hipStream_t stream);
+hipError_t launch_mx4_dequantize(const uint8_t* xq, const uint8_t* x_scale, void* x, int dtype, int M, int K,
+                                 hipStream_t stream);
+struct Mx4GemmArgs {
+    const uint8_t* xq;
+    const uint8_t* x_scale;
+    const uint8_t* wq;
+    const uint8_t* w_scale;
+    const void* bias;         // or null
+    void* y;
+    int M, N, K;
+};
+hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, int dtype, hipStream_t stream);
+
+// ---- rotary positions (vq_rotary.hip) and attention (vq_attention.hip) -----------------------------------------
+struct RotaryArgs {
+    const void* q;
+    void* q_out;
+    const void* k;
+    void* k_out;
+    const int32_t* positions;
+    const float* inv_freq;
+    float amplitude;
+    int T, q_heads, k_heads, head_dim, rot_dim;
+    int64_t q_token, q_head, qo_token, qo_head, k_token, k_head, ko_token, ko_head;   // strides in elements
+    int copied_from, copied, lanes_h;    // the launch's: pieces of a head, and threads that share its heads
+};
+hipError_t launch_rotary(RotaryArgs a, int dtype, int interleaved, hipStream_t stream);
+
+struct AttentionArgs {
+    const void* q;
+    const void* k;
+    const void* v;
+    void* out;
+    const int32_t* cu_q;
+    const int32_t* cu_k;
+    int sequences, Tq, Tk, heads, kv_heads, group, head_dim, causal;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;       // strides in elements
+    float scale_log2;         // softmax_scale / ln 2
+    float* part_o;            // [splits][Tq * heads][head_dim] and [splits][Tq * heads][2]: sums, maxima and weights
+    float* part_ml;
+    int splits;
+};
+// Workgroups that divide the keys of a tile (1: none do), from the sizes alone.
+int attention_splits(int sequences, int Tq, int Tk, int heads, int kv_heads);
+hipError_t launch_attention(const AttentionArgs& a, int dtype, hipStream_t stream);
 
 }  // namespace vq
 

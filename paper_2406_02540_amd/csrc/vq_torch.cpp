@@ -14,12 +14,16 @@
 #include <Python.h>
 
 #include <climits>
+#include <cmath>
 #include <type_traits>
 
 #include <ATen/ATen.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/core/StreamGuard.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/Stream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -55,6 +59,14 @@ struct Entries {
     decltype(&::vq_gelu_linear) gelu_linear;
     decltype(&::vq_residual_linear) residual_linear;
     decltype(&::vq_hadamard_linear) hadamard_linear;
+    decltype(&::vq_mx4_quantize) mx4_quantize;
+    decltype(&::vq_mx4_dequantize) mx4_dequantize;
+    decltype(&::vq_gemm_mx4) gemm_mx4;
+    decltype(&::vq_linear_mx4) linear_mx4;
+    decltype(&::vq_linear_mx4_workspace_bytes) linear_mx4_workspace_bytes;
+    decltype(&::vq_rotary) rotary;
+    decltype(&::vq_attention) attention;
+    decltype(&::vq_attention_workspace_bytes) attention_workspace_bytes;
 } g_lib;
 static_assert(sizeof(Entries) % sizeof(void*) == 0, "a plain array of addresses");
 constexpr Py_ssize_t kEntries = sizeof(Entries) / sizeof(void*);
@@ -585,6 +597,285 @@ PyObject* hadamard_linear(PyObject* const* a) {  // x chan_mul w w_bits w_scale 
     return l.y.release();
 }
 
+// ---- microscaled 4-bit floating point, rotary positions, attention ------------------------------------
+
+// The tensors of a call: of one device, which is the current one while this lives.
+class OnDevice {
+    const c10::Device device_;
+    c10::OptionalDeviceGuard guard_;
+
+  public:
+    explicit OnDevice(const at::Tensor& first) : device_(first.device()) {
+        if (c10::hip::device_count() > 0) guard_.reset_device(device_);
+    }
+    void same(const at::Tensor* t, const char* name) const {
+        if (t && t->device() != device_) {
+            PyErr_Format(PyExc_ValueError, "%s: is on another device than the first argument", name);
+            throw Raised{};
+        }
+    }
+};
+
+vq_dtype type_code(at::ScalarType t, bool f32, const char* name) {
+    if (t == at::kHalf) return VQ_F16;
+    if (t == at::kBFloat16) return VQ_BF16;
+    if (t == at::kFloat && f32) return VQ_F32;
+    PyErr_Format(PyExc_TypeError, f32 ? "%s: expected torch.float16, torch.bfloat16 or torch.float32, got %s"
+                                      : "%s: expected torch.float16 or torch.bfloat16, got %s", name, dtype_name(t));
+    throw Raised{};
+}
+at::ScalarType dtype_argument(PyObject* o) {
+    if (!THPDtype_Check(o)) fail(PyExc_TypeError, "dtype: expected a torch.dtype");
+    return ((THPDtype*)o)->scalar_type;
+}
+
+// A device tensor of any type that the call takes, dense or a view.
+const at::Tensor& some_device_tensor(PyObject* o, const char* name) {
+    if (!THPVariable_Check(o) || !THPVariable_Unpack(o).is_cuda()) {
+        PyErr_Format(PyExc_TypeError, "%s: expected a device tensor", name);
+        throw Raised{};
+    }
+    return THPVariable_Unpack(o);
+}
+const at::Tensor& floating(PyObject* o, bool f32, const char* name) {
+    const at::Tensor& t = some_device_tensor(o, name);
+    type_code(t.scalar_type(), f32, name);
+    return required(o, t.scalar_type(), name);
+}
+
+int fits_int(int64_t v, const char* where) {
+    if (v > INT_MAX) raise_status(VQ_ERR_SHAPE, where);
+    return (int)v;
+}
+int64_t scale_stride(int64_t K) { return (K / 32 + 3) / 4 * 4; }
+
+// Codes [rows, K/2] and their scales; K.
+int64_t check_codes(const at::Tensor& q, const at::Tensor& s, const char* text) {
+    const Rows r = matrix(q);
+    if (!is_matrix(s, r.n, scale_stride(2 * r.k))) fail(PyExc_ValueError, text);
+    return 2 * r.k;
+}
+
+PyObject* mx4_quantize(PyObject* const* a) {  // x chan_mul xq x_scale stream
+    const at::Tensor& x = floating(a[0], true, "x");
+    const OnDevice device(x);
+    const CallStream st(a[4]);
+    const Rows r = matrix(x);
+    const int M = fits_int(r.n, "vq_mx4_quantize"), K = fits_int(r.k, "vq_mx4_quantize");
+    if (K <= 0 || K % 32) raise_status(VQ_ERR_SHAPE, "vq_mx4_quantize");
+    const at::Tensor* cm = channel_vector(a[1], r.k, "chan_mul");
+    device.same(cm, "chan_mul");
+    Output xq(a[2], {r.n, r.k / 2}, at::kByte, "xq", "output shapes", x, st);
+    Output xs(a[3], {r.n, scale_stride(r.k)}, at::kByte, "x_scale", "output shapes", x, st);
+    device.same(&xq.t, "xq");
+    device.same(&xs.t, "x_scale");
+    enqueue("vq_mx4_quantize", g_lib.mx4_quantize, ptr(x), (int)type_code(x.scalar_type(), true, "x"), as<float>(cm),
+            as<uint8_t>(xq.t), as<uint8_t>(xs.t), M, K, st.handle());
+    return tuple_of(xq.release(), xs.release());
+}
+
+PyObject* mx4_dequantize(PyObject* const* a) {  // xq x_scale dtype x stream
+    const at::Tensor& xq = required(a[0], at::kByte, "xq");
+    const OnDevice device(xq);
+    const CallStream st(a[4]);
+    const at::Tensor& xs = required(a[1], at::kByte, "x_scale");
+    device.same(&xs, "x_scale");
+    const int64_t M = matrix(xq).n, K = check_codes(xq, xs, "x_scale must have shape [M, MX4_SCALE_STRIDE(K)]");
+    const at::ScalarType dtype = a[3] == Py_None ? dtype_argument(a[2]) : some_device_tensor(a[3], "x").scalar_type();
+    const int code = type_code(dtype, true, "dtype"), m = fits_int(M, "vq_mx4_dequantize"), k = fits_int(K, "vq_mx4_dequantize");
+    Output x(a[3], {M, K}, dtype, "x", "x must have shape [M,K]", xq, st);
+    device.same(&x.t, "x");
+    enqueue("vq_mx4_dequantize", g_lib.mx4_dequantize, as<uint8_t>(xq), as<uint8_t>(xs), ptr(x.t), code, m, k, st.handle());
+    return x.release();
+}
+
+PyObject* gemm_mx4(PyObject* const* a) {  // xq x_scale wq w_scale bias y dtype stream
+    const at::Tensor& xq = required(a[0], at::kByte, "xq");
+    const OnDevice device(xq);
+    const CallStream st(a[7]);
+    const at::Tensor& xs = required(a[1], at::kByte, "x_scale");
+    const at::Tensor& wq = required(a[2], at::kByte, "wq");
+    const at::Tensor& ws = required(a[3], at::kByte, "w_scale");
+    const int64_t M = matrix(xq).n, K = check_codes(xq, xs, "x_scale must have shape [M, MX4_SCALE_STRIDE(K)]");
+    const int64_t N = matrix(wq).n;
+    if (check_codes(wq, ws, "w_scale must have shape [N, MX4_SCALE_STRIDE(K)]") != K) fail(PyExc_ValueError, "weight shape does not match K");
+    const at::ScalarType dtype = a[5] != Py_None   ? some_device_tensor(a[5], "y").scalar_type()
+                                 : a[4] != Py_None ? some_device_tensor(a[4], "bias").scalar_type()
+                                                   : dtype_argument(a[6]);
+    const int code = type_code(dtype, false, "dtype");
+    const at::Tensor* bias = device_tensor(a[4], dtype, "bias");
+    if (bias && !is_vector(*bias, N)) fail(PyExc_ValueError, "bias must have shape [N]");
+    const int m = fits_int(M, "vq_gemm_mx4"), n = fits_int(N, "vq_gemm_mx4"), k = fits_int(K, "vq_gemm_mx4");
+    Output y(a[5], {M, N}, dtype, "y", "y must have shape [M,N]", xq, st);
+    device.same(&xs, "x_scale");
+    device.same(&wq, "wq");
+    device.same(&ws, "w_scale");
+    device.same(bias, "bias");
+    device.same(&y.t, "y");
+    enqueue("vq_gemm_mx4", g_lib.gemm_mx4, as<uint8_t>(xq), as<uint8_t>(xs), as<uint8_t>(wq), as<uint8_t>(ws), ptr(bias), ptr(y.t),
+            code, m, n, k, st.handle());
+    return y.release();
+}
+
+PyObject* linear_mx4(PyObject* const* a) {  // x chan_mul w w_scale bias y workspace stream
+    const at::Tensor& x = floating(a[0], false, "x");
+    const OnDevice device(x);
+    const CallStream st(a[7]);
+    const Rows r = matrix(x);
+    const at::Tensor* cm = channel_vector(a[1], r.k, "chan_mul");
+    const at::Tensor& wq = required(a[2], at::kByte, "w");
+    const at::Tensor& ws = required(a[3], at::kByte, "w_scale");
+    const int64_t N = matrix(wq).n;
+    if (check_codes(wq, ws, "w_scale must have shape [N, MX4_SCALE_STRIDE(K)]") != r.k) fail(PyExc_ValueError, "weight shape does not match K");
+    const at::Tensor* bias = device_tensor(a[4], x.scalar_type(), "bias");
+    if (bias && !is_vector(*bias, N)) fail(PyExc_ValueError, "bias must have shape [N]");
+    const int M = fits_int(r.n, "vq_linear_mx4"), n = fits_int(N, "vq_linear_mx4"), K = fits_int(r.k, "vq_linear_mx4");
+    Output y(a[5], {r.n, N}, x.scalar_type(), "y", "y must have shape [M,N]", x, st);
+    at::Tensor workspace;
+    if (a[6] == Py_None)
+        workspace = st.empty({std::max<int64_t>((int64_t)g_lib.linear_mx4_workspace_bytes(M, n, K), 16)}, at::kByte, x, false);
+    else
+        workspace = *device_tensor(a[6], at::kByte, "workspace");
+    device.same(cm, "chan_mul");
+    device.same(&wq, "w");
+    device.same(&ws, "w_scale");
+    device.same(bias, "bias");
+    device.same(&y.t, "y");
+    device.same(&workspace, "workspace");
+    enqueue("vq_linear_mx4", g_lib.linear_mx4, ptr(x), as<float>(cm), as<uint8_t>(wq), as<uint8_t>(ws), ptr(bias), ptr(y.t),
+            (int)type_code(x.scalar_type(), false, "x"), ptr(workspace), (size_t)workspace.numel(), M, n, K, st.handle());
+    return y.release();
+}
+
+// A view [tokens, heads, channels] whose channels lie next to each other, and its strides (a single token's or head's is that of a
+// dense view: torch leaves it open).
+struct Heads {
+    const at::Tensor* t;
+    int64_t tokens, heads, channels, token_stride, head_stride;
+    Heads(const at::Tensor& view, const char* name) : t(&view) {
+        if (view.dim() != 3) {
+            PyErr_Format(PyExc_ValueError, "%s: expected [tokens, heads, channels]", name);
+            throw Raised{};
+        }
+        tokens = view.size(0), heads = view.size(1), channels = view.size(2);
+        if (channels > 1 && view.stride(2) != 1) {
+            PyErr_Format(PyExc_ValueError, "%s: the channels of a head must be contiguous", name);
+            throw Raised{};
+        }
+        head_stride = heads > 1 ? view.stride(1) : channels;
+        token_stride = tokens > 1 ? view.stride(0) : heads * channels;
+    }
+};
+Heads heads_argument(PyObject* o, at::ScalarType dtype, const char* name) {
+    const at::Tensor& t = some_device_tensor(o, name);
+    if (t.scalar_type() != dtype) {
+        PyErr_Format(PyExc_TypeError, "%s: expected %s, got %s", name, dtype_name(dtype), dtype_name(t.scalar_type()));
+        throw Raised{};
+    }
+    return Heads(t, name);
+}
+// The output view that belongs to an input: the caller's, or a new dense one (not cleared).
+struct HeadsOutput {
+    PyObject* given = nullptr;
+    at::Tensor t;
+    HeadsOutput() = default;
+    HeadsOutput(PyObject* o, const Heads& like, const char* name, const CallStream& st) {
+        if (o == Py_None) {
+            t = st.empty({like.tokens, like.heads, like.channels}, like.t->scalar_type(), *like.t, true);
+            return;
+        }
+        given = o;
+        const Heads h = heads_argument(o, like.t->scalar_type(), name);
+        if (h.tokens != like.tokens || h.heads != like.heads || h.channels != like.channels) {
+            PyErr_Format(PyExc_ValueError, "%s: another shape than its input", name);
+            throw Raised{};
+        }
+        t = *h.t;
+    }
+    Heads view(const char* name) const { return Heads(t, name); }
+    PyObject* release() {
+        if (given) {
+            Py_INCREF(given);
+            return given;
+        }
+        return THPVariable_Wrap(std::move(t));
+    }
+};
+
+PyObject* rotary(PyObject* const* a) {  // q k positions inv_freq interleaved amplitude q_out k_out stream
+    const at::Tensor& first = some_device_tensor(a[0], "q");
+    const int code = type_code(first.scalar_type(), false, "q");
+    const OnDevice device(first);
+    const CallStream st(a[8]);
+    const Heads q(first, "q");
+    const at::Tensor& positions = required(a[2], at::kInt, "positions");
+    const at::Tensor& freq = required(a[3], at::kFloat, "inv_freq");
+    if (!is_vector(positions, q.tokens)) fail(PyExc_ValueError, "positions must have shape [T]");
+    if (freq.dim() != 1) fail(PyExc_ValueError, "inv_freq must have shape [rot_dim / 2]");
+    const bool has_k = a[1] != Py_None;
+    const Heads k = has_k ? heads_argument(a[1], first.scalar_type(), "k") : q;
+    if (k.tokens != q.tokens || k.channels != q.channels) fail(PyExc_ValueError, "k must have q's tokens and channels");
+    const int interleaved = truth(a[4]);
+    const float amplitude = (float)number(a[5]);
+    if (!has_k && a[7] != Py_None) fail(PyExc_ValueError, "k_out without k");
+    const int T = fits_int(q.tokens, "vq_rotary"), hq = fits_int(q.heads, "vq_rotary"), hk = has_k ? fits_int(k.heads, "vq_rotary") : 0;
+    const int D = fits_int(q.channels, "vq_rotary"), R = fits_int(2 * freq.size(0), "vq_rotary");
+    HeadsOutput qo(a[6], q, "q_out", st), ko;
+    if (has_k) ko = HeadsOutput(a[7], k, "k_out", st);
+    device.same(&positions, "positions");
+    device.same(&freq, "inv_freq");
+    device.same(k.t, "k");
+    device.same(&qo.t, "q_out");
+    if (has_k) device.same(&ko.t, "k_out");
+    const Heads qv = qo.view("q_out"), kv = has_k ? ko.view("k_out") : qv;
+    const int64_t strides[8] = {q.token_stride, q.head_stride, qv.token_stride, qv.head_stride,
+                                k.token_stride, k.head_stride, kv.token_stride, kv.head_stride};
+    enqueue("vq_rotary", g_lib.rotary, ptr(q.t), ptr(qo.t), has_k ? ptr(k.t) : nullptr, has_k ? ptr(ko.t) : nullptr, code,
+            as<int32_t>(positions), as<float>(freq), amplitude, interleaved, T, hq, hk, D, R, (const int64_t*)strides, st.handle());
+    PyObject* const first_out = qo.release();
+    if (has_k) return tuple_of(first_out, ko.release());
+    Py_INCREF(Py_None);
+    return tuple_of(first_out, Py_None);
+}
+
+PyObject* attention(PyObject* const* a) {  // q k v cu_q cu_k softmax_scale causal out workspace stream
+    const at::Tensor& first = some_device_tensor(a[0], "q");
+    const int code = type_code(first.scalar_type(), false, "q");
+    const OnDevice device(first);
+    const CallStream st(a[9]);
+    const Heads q(first, "q"), k = heads_argument(a[1], first.scalar_type(), "k"), v = heads_argument(a[2], first.scalar_type(), "v");
+    if (v.tokens != k.tokens || v.heads != k.heads) fail(PyExc_ValueError, "k and v must have the same tokens and heads");
+    if (k.channels != q.channels || v.channels != q.channels) fail(PyExc_ValueError, "q, k and v must have the same channels");
+    const at::Tensor& cu_q = required(a[3], at::kInt, "cu_q");
+    const at::Tensor& cu_k = required(a[4], at::kInt, "cu_k");
+    if (cu_q.dim() != 1 || cu_q.size(0) < 1 || !is_vector(cu_k, cu_q.size(0))) fail(PyExc_ValueError, "cu_q and cu_k must have shape [sequences + 1]");
+    const float scale = a[5] == Py_None ? (float)(1.0 / std::sqrt((double)std::max<int64_t>(q.channels, 1))) : (float)number(a[5]);
+    const int causal = truth(a[6]);
+    const int B = fits_int(cu_q.size(0) - 1, "vq_attention"), Tq = fits_int(q.tokens, "vq_attention"), Tk = fits_int(k.tokens, "vq_attention");
+    const int H = fits_int(q.heads, "vq_attention"), G = fits_int(k.heads, "vq_attention"), D = fits_int(q.channels, "vq_attention");
+    HeadsOutput out(a[7], q, "out", st);
+    at::Tensor workspace;
+    if (a[8] == Py_None) {
+        const int64_t need = (int64_t)g_lib.attention_workspace_bytes(B, Tq, Tk, H, G, D);
+        if (need > 0) workspace = st.empty({need}, at::kByte, first, false);
+    } else {
+        workspace = *device_tensor(a[8], at::kByte, "workspace");
+        device.same(&workspace, "workspace");
+    }
+    device.same(k.t, "k");
+    device.same(v.t, "v");
+    device.same(&cu_q, "cu_q");
+    device.same(&cu_k, "cu_k");
+    device.same(&out.t, "out");
+    const Heads o = out.view("out");
+    const int64_t strides[8] = {q.token_stride, q.head_stride, k.token_stride, k.head_stride,
+                                v.token_stride, v.head_stride, o.token_stride, o.head_stride};
+    const size_t bytes = workspace.defined() ? (size_t)workspace.numel() : 0;
+    enqueue("vq_attention", g_lib.attention, ptr(q.t), ptr(k.t), ptr(v.t), ptr(out.t), code, as<int32_t>(cu_q), as<int32_t>(cu_k), B, Tq,
+            Tk, H, G, D, (const int64_t*)strides, scale, causal, bytes ? ptr(workspace) : nullptr, bytes, st.handle());
+    return out.release();
+}
+
 // ---- module ------------------------------------------------------------------------------------
 
 // bind(vq_error, addresses): the exception class and the entry points' addresses in Entries' order.
@@ -649,6 +940,12 @@ PyMethodDef g_methods[] = {
     VQ_ENTRY(gelu_linear, 10),
     VQ_ENTRY(residual_linear, 13),
     VQ_ENTRY(hadamard_linear, 9),
+    VQ_ENTRY(mx4_quantize, 5),
+    VQ_ENTRY(mx4_dequantize, 5),
+    VQ_ENTRY(gemm_mx4, 8),
+    VQ_ENTRY(linear_mx4, 8),
+    VQ_ENTRY(rotary, 9),
+    VQ_ENTRY(attention, 10),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_vq_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,89 @@
+"""Rotary positions against the formula in 64 bits."""
+import pytest
+import torch
+
+import paper_2406_02540_amd as vq
+import operator_util as ou
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = ou.F16, ou.BF16
+
+
+def _views(T, H, G, D, dtype, seed=0):
+    g = torch.Generator().manual_seed(seed + 7 * T + D)
+    buf = torch.randn(T, H + 2 * G, D, generator=g).to(dtype).cuda()
+    return buf, buf[:, :H], buf[:, H:H + G]
+
+
+def _check(got, x, p, f, interleaved, amplitude, what):
+    want, off = ou.rotary(x, p, f, interleaved, amplitude)
+    R = 2 * f.shape[0]
+    ou.check(got[..., :R], want[..., :R], off[..., :R] + ou.HALF[x.dtype] * want[..., :R].abs() + ou.TINY[x.dtype], what)
+    assert torch.equal(got[..., R:], x[..., R:])
+
+
+@pytest.mark.parametrize("T,H,G,D,R", [(1, 1, 1, 8, 8), (1, 32, 8, 128, 64), (7, 3, 1, 64, 64), (100, 16, 16, 72, 72),
+                                       (33, 5, 5, 80, 16), (513, 4, 2, 96, 40), (3000, 16, 16, 72, 72)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_slices(T, H, G, D, R, interleaved, dtype):
+    buf, q, k = _views(T, H, G, D, dtype)
+    kept = buf.clone()
+    g = torch.Generator().manual_seed(T)
+    p = torch.randint(-(1 << 20), 1 << 20, (T,), generator=g, dtype=torch.int32).cuda()
+    f, _ = vq.vq_rotary_frequencies(R)
+    f = f.cuda()
+    qo, ko = vq.vq_rotary(q, k, p, f, interleaved=interleaved, amplitude=1.25)
+    assert torch.equal(buf, kept) and qo.is_contiguous() and ko.is_contiguous()
+    _check(qo, q, p, f, interleaved, 1.25, "q")
+    _check(ko, k, p, f, interleaved, 1.25, "k")
+    # in place: the same numbers, the rest of the buffer as it was
+    vq.vq_rotary(q, k, p, f, interleaved=interleaved, amplitude=1.25, q_out=q, k_out=k)
+    assert torch.equal(q, qo) and torch.equal(k, ko) and torch.equal(buf[:, H + G:], kept[:, H + G:])
+    alone, none = vq.vq_rotary(kept[:, :H], None, p, f, interleaved=interleaved, amplitude=1.25)
+    assert none is None and torch.equal(alone, qo)
+
+
+def test_positions_at_the_ends_of_their_range():
+    p = torch.tensor([0, 1, -1, 2**31 - 1, -2**31, 2**30 + 1], dtype=torch.int32).cuda()
+    _, q, k = _views(6, 2, 1, 64, F16)
+    f, _ = vq.vq_rotary_frequencies(64)
+    f = f.cuda()
+    qo, ko = vq.vq_rotary(q, k, p, f)
+    _check(qo, q, p, f, False, 1.0, "far")
+    assert torch.equal(qo[0], q[0])
+    # the negative position undoes it, but for two roundings
+    back, _ = vq.vq_rotary(qo[:4], None, torch.tensor([0, -1, 1, 1 - 2**31], dtype=torch.int32).cuda(), f)
+    assert ((back - q[:4]).abs() <= 4 * 2.0 ** -11 * 8).all()
+
+
+def test_head_major_and_shared_views():
+    T, H, D = 50, 4, 64
+    base = torch.randn(H, T, D, generator=torch.Generator().manual_seed(1)).to(BF16).cuda()
+    q = base.transpose(0, 1)                                  # [T,H,D], heads outermost in memory
+    one = torch.randn(T, 1, D, generator=torch.Generator().manual_seed(2)).to(BF16).cuda().expand(T, 3, D)
+    p = torch.arange(T, dtype=torch.int32).cuda()
+    f, _ = vq.vq_rotary_frequencies(D)
+    f = f.cuda()
+    out = torch.empty(H, T, D, dtype=BF16, device="cuda").transpose(0, 1)
+    qo, ko = vq.vq_rotary(q, one, p, f, q_out=out)
+    _check(out, q, p, f, False, 1.0, "head-major")
+    _check(ko, one, p, f, False, 1.0, "shared")
+
+
+def test_captured_and_replayed():
+    buf, q, k = _views(200, 8, 2, 128, F16)
+    f, _ = vq.vq_rotary_frequencies(128)
+    f = f.cuda()
+    p = torch.arange(200, dtype=torch.int32).cuda()
+    qo, ko = torch.empty(200, 8, 128, dtype=F16, device="cuda"), torch.empty(200, 2, 128, dtype=F16, device="cuda")
+    vq.vq_rotary(q, k, p, f, q_out=qo, k_out=ko)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vq.vq_rotary(q, k, p, f, q_out=qo, k_out=ko)
+    for shift in (1000, 0, 77):
+        p.copy_(torch.arange(200, dtype=torch.int32) + shift)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = vq.vq_rotary(q, k, p, f)
+        assert torch.equal(qo, want[0]) and torch.equal(ko, want[1])
