@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256) void attention_join(AttentionArgs a) {
 }
 
 template <class TYPE>
-hipError_t launch(const AttentionArgs& a, hipStream_t stream) {
+hipError_t launch_rows(const AttentionArgs& a, hipStream_t stream) {
     const long blocks = (long)a.sequences * a.splits * a.kv_heads;
     constexpr int WAVES = 4;
     if (blocks * 64 * WAVES >= 1l << 32) return hipErrorInvalidValue;
@@ -209,25 +209,30 @@ hipError_t launch(const AttentionArgs& a, hipStream_t stream) {
                                     : a.head_dim <= 80 ? attention_rows<TYPE, 12, 5, WAVES>
                                     : a.head_dim <= 96 ? attention_rows<TYPE, 12, 6, WAVES>
                                                        : attention_rows<TYPE, 16, 8, WAVES>;
-    hipError_t e = enqueue(kernel, dim3((unsigned)blocks), dim3(64 * WAVES), stream, a);
-    if (e != hipSuccess || a.splits == 1) return e;
-    const long join = ((long)a.Tq * a.heads * (a.head_dim / 8) + 255) / 256;
-    return enqueue(attention_join<TYPE>, dim3((unsigned)(join < 1 << 20 ? join : 1 << 20)), dim3(256), stream, a);
+    return enqueue(kernel, dim3((unsigned)blocks), dim3(64 * WAVES), stream, a);
 }
 
 }  // namespace
 
 int attention_splits(int sequences, int Tq, int Tk, int heads, int kv_heads) {
-    if ((long)Tq * (heads / kv_heads) > 32l * sequences) return 1;
-    // a part of at least 512 keys of the average sequence, and workgroups for four turns of the chip
-    const long items = (long)sequences * kv_heads, keys = (long)Tk / sequences;
-    long splits = 1024 / items;
+    const int group = heads / kv_heads;
+    const long keys = (long)Tk / sequences;
+    const bool rows = attention_by_rows(sequences, Tq, group);
+    // parts of at least 512 keys of the average sequence, and workgroups for four turns of the chip, or one of tiles
+    const long items = (rows ? (long)sequences : attention_items(sequences, Tq, group)) * kv_heads;
+    long splits = (rows ? 1024 : 512) / items;
     if (splits > keys / 512) splits = keys / 512;
     return splits < 1 ? 1 : splits > 64 ? 64 : (int)splits;
 }
 
 hipError_t launch_attention(const AttentionArgs& a, int dtype, hipStream_t stream) {
-    return dtype == VQ_F16 ? launch<F16>(a, stream) : launch<BF16>(a, stream);
+    const hipError_t e = !attention_by_rows(a.sequences, a.Tq, a.group) ? launch_attention_tiles(a, dtype, stream)
+                         : dtype == VQ_F16                              ? launch_rows<F16>(a, stream)
+                                                                        : launch_rows<BF16>(a, stream);
+    if (e != hipSuccess || a.splits == 1) return e;
+    const long join = ((long)a.Tq * a.heads * (a.head_dim / 8) + 255) / 256;
+    return enqueue(dtype == VQ_F16 ? attention_join<F16> : attention_join<BF16>, dim3((unsigned)(join < 1 << 20 ? join : 1 << 20)),
+                   dim3(256), stream, a);
 }
 
 }  // namespace vq

@@ -120,10 +120,17 @@ struct AttentionArgs {
     float* part_o;            // [splits][Tq * heads][head_dim] and [splits][Tq * heads][2]: sums, maxima and weights
     float* part_ml;
     int splits;
+    long items;               // attention_items(): tiles of query rows, the launch's
 };
 // Workgroups that divide the keys of a tile (1: none do), from the sizes alone.
 int attention_splits(int sequences, int Tq, int Tk, int heads, int kv_heads);
 hipError_t launch_attention(const AttentionArgs& a, int dtype, hipStream_t stream);
+// Its two kernels: few query rows a sequence (vq_attention.hip), or tiles of kTileRows (vq_attention_tiles.hip), at most
+// attention_items() of them for a head of K and V.
+constexpr int kTileRows = 128;
+inline bool attention_by_rows(int sequences, int Tq, int group) { return (long)Tq * group <= 32l * sequences; }
+inline long attention_items(int sequences, int Tq, int group) { return (long)Tq * group / kTileRows + sequences; }
+hipError_t launch_attention_tiles(const AttentionArgs& a, int dtype, hipStream_t stream);
 
 }  // namespace vq
 
