@@ -500,9 +500,10 @@ int vq_gemm_mx4(const uint8_t* xq, const uint8_t* x_scale, const uint8_t* wq, co
     const int v = validate_mx4_gemm(xq, x_scale, wq, w_scale, bias, y, dtype, M, N, K);
     if (v != VQ_OK) return v;
     if (M == 0 || N == 0) return VQ_OK;
-    const int arch = check_arch();
+    int num_cus = 0;
+    const int arch = check_arch(&num_cus);
     if (arch != VQ_OK) return arch;
-    return launch_status(vq::launch_mx4_gemm({xq, x_scale, wq, w_scale, bias, y, M, N, K}, dtype, (hipStream_t)hip_stream));
+    return launch_status(vq::launch_mx4_gemm({xq, x_scale, wq, w_scale, bias, y, M, N, K, nullptr, nullptr}, dtype, num_cus, (hipStream_t)hip_stream));
 }
 
 size_t vq_linear_mx4_workspace_bytes(int M, int N, int K) {
@@ -522,11 +523,14 @@ int vq_linear_mx4(const void* x, const float* chan_mul, const uint8_t* wq, const
     uint8_t* const x_scale = xq + round_up((size_t)M * (size_t)(K / 2), kAlign);
     int v = validate_mx4_gemm(xq, x_scale, wq, w_scale, bias, y, dtype, M, N, K);
     if (v != VQ_OK) return v;
-    const int arch = check_arch();
+    int num_cus = 0;
+    const int arch = check_arch(&num_cus);
     if (arch != VQ_OK) return arch;
+    if (vq::small_mx4_layer(M, N, K))
+        return launch_status(vq::launch_mx4_layer_small({nullptr, nullptr, wq, w_scale, bias, y, M, N, K, x, chan_mul}, dtype, (hipStream_t)hip_stream));
     v = launch_status(vq::launch_mx4_quantize(x, dtype, chan_mul, xq, x_scale, M, K, (hipStream_t)hip_stream));
     if (v != VQ_OK) return v;
-    return launch_status(vq::launch_mx4_gemm({xq, x_scale, wq, w_scale, bias, y, M, N, K}, dtype, (hipStream_t)hip_stream));
+    return launch_status(vq::launch_mx4_gemm({xq, x_scale, wq, w_scale, bias, y, M, N, K, nullptr, nullptr}, dtype, num_cus, (hipStream_t)hip_stream));
 }
 
 int vq_rotary(const void* q, void* q_out, const void* k, void* k_out, int dtype, const int32_t* positions,

@@ -89,8 +89,18 @@ struct Mx4GemmArgs {
     const void* bias;         // or null
     void* y;
     int M, N, K;
+    const void* x;            // launch_mx4_layer_small: the activations, and their factors or null
+    const float* chan_mul;
 };
-hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, int dtype, hipStream_t stream);
+// The kernel that a product takes: tiles of tokens x channels, shared by their wavefronts (vq_mx4_gemm.hip) or with the wavefronts
+// dividing K (vq_mx4_gemm_split.hip: 32 x 32, 48 x 48, 32 x 64).
+struct Mx4Choice { int tile_t, tile_c; bool divide_k; };
+Mx4Choice choose_mx4_gemm(int M, int N, int K, int num_cus);
+hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, int dtype, int num_cus, hipStream_t stream);
+hipError_t launch_mx4_gemm_lines(int tile_t, int tile_c, const Mx4GemmArgs& a, int dtype, hipStream_t stream);
+// A layer of few tokens in one launch, from x instead of xq; small_mx4_layer: whether it is the faster way.
+bool small_mx4_layer(int M, int N, int K);
+hipError_t launch_mx4_layer_small(const Mx4GemmArgs& a, int dtype, hipStream_t stream);
 
 // ---- rotary positions (vq_rotary.hip) and attention (vq_attention.hip) -----------------------------------------
 struct RotaryArgs {

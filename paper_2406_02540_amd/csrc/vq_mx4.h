@@ -19,6 +19,12 @@ __device__ __forceinline__ int mx_scale_of(unsigned top) {
     return e == 255 ? kMxNan : max(e - 2, 0);
 }
 
+// Four neighbouring lanes hold a block: the largest of their numbers.
+__device__ __forceinline__ unsigned largest_of_block(unsigned top) {
+    top = max(top, (unsigned)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xF, 0xF, true));          // the neighbour's
+    return max(top, (unsigned)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xF, 0xF, true));         // the other pair's
+}
+
 // Eight values of a block as codes, the first in the lowest bits.  The conversion divides by the power of two in
 // `scale`'s exponent, rounds to nearest even and saturates.
 __device__ __forceinline__ unsigned mx_encode(const float* t, int byte) {

@@ -88,8 +88,7 @@ __global__ __launch_bounds__(kThreads) void mx4_quantize(MxArgs a) {
                 if (MASK) t[i] *= mul[i];
                 top = max(top, magnitude(t[i]));
             }
-            top = max(top, (unsigned)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xF, 0xF, true));   // neighbour
-            top = max(top, (unsigned)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xF, 0xF, true));   // the other pair
+            top = largest_of_block(top);
             const int byte = mx_scale_of(top);
             const size_t row = (size_t)p.group * kRows + r;
             *(unsigned*)(a.xq + row * (a.K / 2) + 4 * p.piece) = mx_encode(t, byte);
