@@ -593,7 +593,8 @@ size_t vq_attention_workspace_bytes(int sequences, int Tq, int Tk, int heads, in
     if (sequences <= 0 || Tq <= 0 || Tk < 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0 || head_dim <= 0 ||
         head_dim % 8 != 0 || head_dim > VQ_MAX_HEAD_DIM)
         return 0;
-    const size_t parts = (size_t)vq::attention_splits(sequences, Tq, Tk, heads, kv_heads);
+    if ((int64_t)Tq * heads > 0x7FFFFFFF) return 0;
+    const size_t parts = (size_t)1 << vq::attention_split_shift(sequences, Tq, Tk, heads, kv_heads);
     return parts == 1 ? 0 : parts * (size_t)Tq * (size_t)heads * (size_t)(head_dim + 2) * sizeof(float);
 }
 
@@ -602,7 +603,7 @@ int vq_attention(const void* q, const void* k, const void* v, void* out, int dty
                  float softmax_scale, int causal, void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
     if (sequences < 0 || Tq < 0 || Tk < 0 || heads <= 0 || kv_heads <= 0 || heads > 1 << 16 || heads % kv_heads != 0 ||
-        head_dim <= 0 || head_dim % 8 != 0 || head_dim > VQ_MAX_HEAD_DIM || (causal != 0 && causal != 1) ||
+        (int64_t)Tq * heads > 0x7FFFFFFF || head_dim <= 0 || head_dim % 8 != 0 || head_dim > VQ_MAX_HEAD_DIM || (causal != 0 && causal != 1) ||
         !std::isfinite(softmax_scale) || !(softmax_scale > 0.0f))
         return VQ_ERR_SHAPE;
     if (sequences == 0 || Tq == 0) return VQ_OK;
@@ -629,9 +630,10 @@ int vq_attention(const void* q, const void* k, const void* v, void* out, int dty
     a.q_token = strides[0], a.q_head = strides[1], a.k_token = strides[2], a.k_head = strides[3];
     a.v_token = strides[4], a.v_head = strides[5], a.o_token = strides[6], a.o_head = strides[7];
     a.scale_log2 = (float)((double)softmax_scale * 1.44269504088896340736);
-    a.splits = vq::attention_splits(sequences, Tq, Tk, heads, kv_heads);
+    a.group_shift = (a.group & (a.group - 1)) == 0 ? __builtin_ctz(a.group) : -1;
+    a.split_shift = vq::attention_split_shift(sequences, Tq, Tk, heads, kv_heads);
     a.part_o = (float*)workspace;
-    a.part_ml = a.part_o ? a.part_o + (size_t)a.splits * Tq * heads * head_dim : nullptr;
+    a.part_ml = a.part_o ? a.part_o + ((size_t)Tq << a.split_shift) * heads * head_dim : nullptr;
     return launch_status(vq::launch_attention(a, dtype, (hipStream_t)hip_stream));
 }
 

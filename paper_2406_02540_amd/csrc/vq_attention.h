@@ -37,6 +37,18 @@ __device__ __forceinline__ Span span_of(const AttentionArgs& a, int b) {
     return s;
 }
 
+__device__ __forceinline__ int token_of(const AttentionArgs& a, int row) {
+    return a.group_shift >= 0 ? row >> a.group_shift : (int)((unsigned)row / (unsigned)a.group);
+}
+// Keys of its sequence that a token sees.
+__device__ __forceinline__ int keys_seen(const AttentionArgs& a, const Span& s, int token) {
+    return a.causal ? min(s.m, max(0, s.m - s.n + token + 1)) : s.m;
+}
+// Tiles of keys of a workgroup among those that divide `tiles` (less than 2^26 of them; at most 2^6 workgroups).
+__device__ __forceinline__ int split_begin(const AttentionArgs& a, int tiles, int split) {
+    return (int)((unsigned)tiles * (unsigned)split >> a.split_shift);
+}
+
 // ---- tiles of K and V in LDS ---------------------------------------------------------------------------------
 // [key][CHUNKS of 16 bytes], the chunk of a key at chunk ^ swizzle(key), so that what the LDS serves at once lies in different banks:
 // K is read 16 bytes a lane, one chunk of 32 keys at a time (sixteen lanes are served together: keys 0-3, 12-15 and 20-27, or the
@@ -106,6 +118,40 @@ __device__ __forceinline__ v8s read_v(lds_bytes tile, int key0, int block, int l
 
 // The key of register r of a block of S^T, less the block's first.
 __device__ __forceinline__ constexpr int key_of(int r) { return (r & 3) + 8 * (r >> 2); }   // + 4 (lane / 32)
+
+// A wavefront's 32 rows of outputs, whose lanes' sums l and outputs o (relative to ref) are complete: normalised to `out`, or as they are
+// to the parts.  `row`: token (of all) and head of the lane's row.
+template <class TYPE, int BLOCKS>
+__device__ __forceinline__ void write_rows(const AttentionArgs& a, const v16f* o, float ref, float l, int token, int head, int split, bool real, int half) {
+    typedef typename TYPE::T T;
+    if (a.split_shift == 0) {
+        const float inv = l > 0 ? 1.0f / l : 0.0f;
+        T* const y = (T*)a.out + token * a.o_token + head * a.o_head;
+#pragma unroll
+        for (int c = 0; c < BLOCKS; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+                // a lane has four channels of every eight, the other half of the wavefront the rest: one takes this eight, one the next
+                const unsigned x0 = TYPE::pack(o[c][4 * i] * inv, o[c][4 * i + 1] * inv), x1 = TYPE::pack(o[c][4 * i + 2] * inv, o[c][4 * i + 3] * inv);
+                const unsigned y0 = TYPE::pack(o[c][4 * i + 4] * inv, o[c][4 * i + 5] * inv), y1 = TYPE::pack(o[c][4 * i + 6] * inv, o[c][4 * i + 7] * inv);
+                const auto s0 = __builtin_amdgcn_permlane32_swap(x0, y0, false, false);
+                const auto s1 = __builtin_amdgcn_permlane32_swap(x1, y1, false, false);
+                const int at = 32 * c + 8 * (i + half);
+                if (real && at < a.head_dim) *(v4i*)(y + at) = v4i{(int)s0[0], (int)s1[0], (int)s0[1], (int)s1[1]};
+            }
+    } else if (real) {
+        const size_t slot = ((size_t)split * a.Tq + token) * a.heads + head;
+        float* const y = a.part_o + slot * a.head_dim;
+#pragma unroll
+        for (int c = 0; c < BLOCKS; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = 32 * c + 8 * i + 4 * half;
+                if (at < a.head_dim) *(v4f*)(y + at) = v4f{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
+            }
+        if (half == 0) *(v2f*)(a.part_ml + slot * 2) = v2f{l > 0 ? ref : -__builtin_inff(), l};
+    }
+}
 
 __device__ __forceinline__ float other_half(float v) {
     const unsigned u = __builtin_bit_cast(unsigned, v);

@@ -12,9 +12,9 @@ constexpr float kSlack = 8.0f;    // base 2: how far a score may exceed the refe
 // Tiles of all sequences are numbered so that a sequence's first is floor(cu * group / rows) + b, at least the tiles of the
 // sequences in front of it (floor(x + y) - floor(x) + 1 >= ceil(y)): a sequence is found by bisection, and a number that no tile has
 // is a workgroup that ends at once.
-__device__ __forceinline__ int find_sequence(const AttentionArgs& a, long item, long& tile) {
+__device__ __forceinline__ int find_sequence(const AttentionArgs& a, int item, int& tile) {
     int lo = 0, hi = a.sequences - 1;
-    auto first = [&](int b) { return (long)min(max(a.cu_q[b], 0), a.Tq) * a.group / kTileRows + b; };
+    auto first = [&](int b) { return (int)((unsigned)(min(max(a.cu_q[b], 0), a.Tq) * a.group) / kTileRows) + b; };
     while (lo < hi) {
         const int mid = lo + (hi - lo + 1) / 2;
         if (first(mid) <= item) lo = mid;
@@ -34,12 +34,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tiles(AttentionArgs 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int kv = (int)(blockIdx.x % (unsigned)a.kv_heads);
     const unsigned rest = blockIdx.x / (unsigned)a.kv_heads;
-    const int split = (int)(rest % (unsigned)a.splits);
-    long tile;
+    const int split = (int)rest & ((1 << a.split_shift) - 1);
+    int tile;
     // (the last tiles of a sequence see the most keys: they go first)
-    const int b = find_sequence(a, a.items - 1 - rest / (unsigned)a.splits, tile);
+    const int b = find_sequence(a, a.items - 1 - (int)(rest >> a.split_shift), tile);
     const Span s = span_of(a, b);
-    const long rows = (long)s.n * a.group, row0 = tile * kTileRows;
+    const int rows = s.n * a.group, row0 = tile * kTileRows;
     if (tile < 0 || row0 >= rows) return;
     const int head_bytes = 2 * a.head_dim;
     const T* const k = (const T*)a.k + s.k0 * a.k_token + kv * a.k_head;
@@ -47,16 +47,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tiles(AttentionArgs 
     const int k_stride = (int)(2 * a.k_token), v_stride = (int)(2 * a.v_token);
     const unsigned base = (unsigned)(uintptr_t)(lds_bytes)lds;
 
-    const long r = min(row0 + 32 * wave + (lane & 31), rows - 1);
+    const int r = min(row0 + 32 * wave + (lane & 31), rows - 1);
     const bool real = row0 + 32 * wave + (lane & 31) < rows;
-    const int token = (int)(r / a.group), head = kv * a.group + (int)(r - (long)token * a.group);
-    // keys that a token sees: this lane's row's, the wavefront's fewest, the workgroup's most
-    auto sees = [&](long t) { return a.causal ? (int)min((long)s.m, max(0l, (long)s.m - s.n + t + 1)) : s.m; };
-    const int visible = sees(token);
-    const int least = __builtin_amdgcn_readfirstlane(sees(min(row0 + 32 * wave, rows - 1) / a.group));
-    const int end = sees((min(row0 + kTileRows, rows) - 1) / a.group);
+    const int token = token_of(a, r), head = kv * a.group + r - token * a.group;
+    // keys: this lane's row's, the wavefront's fewest, the workgroup's most
+    const int visible = keys_seen(a, s, token);
+    const int least = __builtin_amdgcn_readfirstlane(keys_seen(a, s, token_of(a, min(row0 + 32 * wave, rows - 1))));
+    const int end = __builtin_amdgcn_readfirstlane(keys_seen(a, s, token_of(a, min(row0 + kTileRows, rows) - 1)));
     const int tiles = (end + kKeys - 1) / kKeys;
-    const int t0 = (int)((long)tiles * split / a.splits), t1 = (int)((long)tiles * (split + 1) / a.splits);
+    const int t0 = split_begin(a, tiles, split), t1 = split_begin(a, tiles, split + 1);
 
     auto ask = [&](int t, int to) {
         const int left = s.m - t * kKeys;
@@ -133,40 +132,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attention_tiles(AttentionArgs 
         }
     }
     l += other_half(l);
-    if (a.splits == 1) {
-        const float inv = l > 0 ? 1.0f / l : 0.0f;
-        T* const y = (T*)a.out + (s.q0 + token) * a.o_token + head * a.o_head;
-#pragma unroll
-        for (int c = 0; c < BLOCKS; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-                // a lane has four channels of every eight, the other half of the wavefront the rest: one takes this eight, one the next
-                unsigned x0 = TYPE::pack(o[c][4 * i] * inv, o[c][4 * i + 1] * inv), x1 = TYPE::pack(o[c][4 * i + 2] * inv, o[c][4 * i + 3] * inv);
-                unsigned y0 = TYPE::pack(o[c][4 * i + 4] * inv, o[c][4 * i + 5] * inv), y1 = TYPE::pack(o[c][4 * i + 6] * inv, o[c][4 * i + 7] * inv);
-                const auto s0 = __builtin_amdgcn_permlane32_swap(x0, y0, false, false);
-                const auto s1 = __builtin_amdgcn_permlane32_swap(x1, y1, false, false);
-                const int at = 32 * c + 8 * (i + half);
-                if (real && at < a.head_dim) *(v4i*)(y + at) = v4i{(int)s0[0], (int)s1[0], (int)s0[1], (int)s1[1]};
-            }
-    } else if (real) {
-        const size_t slot = ((size_t)split * a.Tq + s.q0 + token) * a.heads + head;
-        float* const y = a.part_o + slot * a.head_dim;
-#pragma unroll
-        for (int c = 0; c < BLOCKS; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = 32 * c + 8 * i + 4 * half;
-                if (at < a.head_dim) *(v4f*)(y + at) = v4f{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
-            }
-        if (half == 0) *(v2f*)(a.part_ml + slot * 2) = v2f{l > 0 ? ref : -kInf, l};
-    }
+    write_rows<TYPE, BLOCKS>(a, o, ref, l, s.q0 + token, head, split, real, half);
 }
 
 template <class TYPE>
 hipError_t launch(AttentionArgs a, hipStream_t stream) {
-    a.items = attention_items(a.sequences, a.Tq, a.group);
-    const long blocks = a.items * a.splits * a.kv_heads;
-    if (blocks * 64 * kWaves >= 1l << 32) return hipErrorInvalidValue;
+    const long items = attention_items(a.sequences, a.Tq, a.group), blocks = (items << a.split_shift) * a.kv_heads;
+    a.items = (int)items;
+    if (items > 0x7FFFFFFF || blocks * 64 * kWaves >= 1l << 32) return hipErrorInvalidValue;
     void (*kernel)(AttentionArgs) = a.head_dim <= 64   ? attention_tiles<TYPE, 8, 4>
                                     : a.head_dim <= 80 ? attention_tiles<TYPE, 12, 5>
                                     : a.head_dim <= 96 ? attention_tiles<TYPE, 12, 6>

@@ -124,16 +124,17 @@ struct AttentionArgs {
     void* out;
     const int32_t* cu_q;
     const int32_t* cu_k;
-    int sequences, Tq, Tk, heads, kv_heads, group, head_dim, causal;
+    int sequences, Tq, Tk, heads, kv_heads, head_dim, causal;
+    int group, group_shift;   // heads / kv_heads, and its logarithm if it is a power of two, else -1
     int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;       // strides in elements
     float scale_log2;         // softmax_scale / ln 2
     float* part_o;            // [splits][Tq * heads][head_dim] and [splits][Tq * heads][2]: sums, maxima and weights
     float* part_ml;
-    int splits;
-    long items;               // attention_items(): tiles of query rows, the launch's
+    int split_shift;          // 2^split_shift workgroups divide the keys of a tile
+    int items;                // attention_items(): tiles of query rows, the launch's
 };
-// Workgroups that divide the keys of a tile (1: none do), from the sizes alone.
-int attention_splits(int sequences, int Tq, int Tk, int heads, int kv_heads);
+// The logarithm of the workgroups that divide the keys of a tile, from the sizes alone.  Tq * heads < 2^31.
+int attention_split_shift(int sequences, int Tq, int Tk, int heads, int kv_heads);
 hipError_t launch_attention(const AttentionArgs& a, int dtype, hipStream_t stream);
 // Its two kernels: few query rows a sequence (vq_attention.hip), or tiles of kTileRows (vq_attention_tiles.hip), at most
 // attention_items() of them for a head of K and V.
