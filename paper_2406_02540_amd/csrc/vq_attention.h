@@ -21,6 +21,7 @@ namespace vq {
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char* lds_bytes;
 
 // ---- sequences -----------------------------------------------------------------------------------------------
 
@@ -64,22 +65,33 @@ __device__ __forceinline__ int v_swizzle(int key) {
 
 constexpr int kBehind = 0x7FFFFFF0;        // an offset that no buffer reaches: its lanes load zeros
 
-// Asks for KEYS rows of K or V, THREADS threads together.  `base` is the first of them, keys at or behind `left` and channels
-// behind the head's come as zeros.  A row's stride is at most 2^24 bytes.
+// What a thread loads of KEYS rows of K or V, THREADS threads together.  Rows are at most 2^24 bytes apart.
 template <int CHUNKS, int KEYS, int THREADS, bool IS_V>
-__device__ __forceinline__ void load_tile(const void* base, unsigned lds, int stride, int left, int head_bytes, int thread) {
+struct TileLoader {
     static_assert(KEYS * CHUNKS % THREADS == 0, "whole turns");
-    const v4i rsrc = make_rsrc(base, 0x7FFFFF00u);
-    const unsigned wave_lds = __builtin_amdgcn_readfirstlane(lds + (thread & ~63) * 16);
+    static constexpr int kTurns = KEYS * CHUNKS / THREADS;
+    int at[kTurns];          // from the tile's first row; kBehind behind the head's channels
+    __device__ __forceinline__ TileLoader(int stride, int head_bytes, int thread) {
 #pragma unroll
-    for (int i = 0; i < KEYS * CHUNKS / THREADS; ++i) {
-        const int p = i * THREADS + thread;
-        const int key = p / CHUNKS, slot = p % CHUNKS;
-        const int c = slot ^ (IS_V ? v_swizzle<CHUNKS>(key) : k_swizzle<CHUNKS>(key));
-        const int at = key < left && 16 * c < head_bytes ? key * stride + 16 * c : kBehind;
-        load_to_lds_16(rsrc, wave_lds + i * THREADS * 16, at, 0);
+        for (int i = 0; i < kTurns; ++i) {
+            const int p = i * THREADS + thread, key = p / CHUNKS, slot = p % CHUNKS;
+            const int c = slot ^ (IS_V ? v_swizzle<CHUNKS>(key) : k_swizzle<CHUNKS>(key));
+            at[i] = opaque(16 * c < head_bytes ? key * stride + 16 * c : kBehind);
+        }
     }
-}
+    // Asks for the rows from `base` on, into LDS from `lds` (this wavefront's share: its first thread's 16 bytes).  Rows from `left` on come
+    // as zeros.  KEEP: what lies behind the head's channels in LDS stays.
+    template <bool KEEP = false>
+    __device__ __forceinline__ void ask(const void* base, unsigned lds, int left, int thread) const {
+        const v4i rsrc = make_rsrc(base, 0x7FFFFF00u);
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            if (KEEP && at[i] == kBehind) continue;
+            if (left >= KEYS) load_to_lds_16(rsrc, lds + i * THREADS * 16, at[i], 0);
+            else load_to_lds_16(rsrc, lds + i * THREADS * 16, (i * THREADS + thread) / CHUNKS < left ? at[i] : kBehind, 0);
+        }
+    }
+};
 
 template <class TYPE>
 __device__ __forceinline__ v16f mfma(v8s a, v8s b, v16f c);
@@ -94,27 +106,46 @@ __device__ __forceinline__ v16f mfma<BF16>(v8s a, v8s b, v16f c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
 }
 
-typedef __attribute__((address_space(3))) char* lds_bytes;
+// Where a lane reads K: rows `lane % 32` of 32 keys, channels 16 step + 8 (lane / 32) .. + 7.  The swizzle is an exclusive or on the
+// chunk's number: with 12 chunks on its lower two bits, so that the steps are two places and constants; otherwise a place for every step.
+template <int CHUNKS, int STEPS>
+struct KeyReader {
+    static constexpr int kPlaces = CHUNKS == 12 ? 2 : STEPS;
+    lds_bytes at[kPlaces];
+    __device__ __forceinline__ KeyReader(lds_bytes tile, int lane) {
+        const int key = lane & 31, half = lane >> 5, s = k_swizzle<CHUNKS>(key);
+#pragma unroll
+        for (int i = 0; i < kPlaces; ++i)
+            at[i] = (lds_bytes)(uintptr_t)(unsigned)opaque((int)(unsigned)(uintptr_t)(tile + key * CHUNKS * 16 + ((2 * i + half) ^ s) * 16));
+    }
+    // 32 keys from key0, of a tile `offset` bytes behind the one named above
+    __device__ __forceinline__ v8s read(int offset, int key0, int step) const {
+        lds_bytes const p = CHUNKS == 12 ? at[step & 1] + 64 * (step >> 1) : at[CHUNKS == 12 ? 0 : step];
+        return *(__attribute__((address_space(3))) v8s*)(p + offset + key0 * CHUNKS * 16);
+    }
+};
 
-// Rows `lane % 32` of the 32 keys from `key0`, channels 16 step + 8 (lane / 32) .. + 7.
+// And V, transposed: channel 32 block + lane % 32 of keys key0 + 4h .. + 3 and key0 + 8 + 4h .. + 3, h = lane / 32.  In a transposed
+// read sixteen lanes name four rows of sixteen channels, four lanes a row, and each receives a column.
 template <int CHUNKS>
-__device__ __forceinline__ v8s read_k(lds_bytes tile, int key0, int step, int lane) {
-    const int key = key0 + (lane & 31), c = (2 * step + (lane >> 5)) ^ k_swizzle<CHUNKS>(key);
-    return *(__attribute__((address_space(3))) v8s*)(tile + (key * CHUNKS + c) * 16);
-}
-
-// Channel 32 block + lane % 32 of keys key0 + 4h .. + 3 and key0 + 8 + 4h .. + 3, h = lane / 32.  In a transposed read sixteen
-// lanes name four rows of sixteen channels, four lanes a row, and each receives a column.
-template <int CHUNKS>
-__device__ __forceinline__ v8s read_v(lds_bytes tile, int key0, int block, int lane) {
-    const int in16 = lane & 15;
-    const int key = key0 + 4 * (lane >> 5) + (in16 >> 2), c = 4 * block + 2 * (lane >> 4 & 1) + (in16 >> 1 & 1);
-    lds_bytes at = tile + (key * CHUNKS + (c ^ v_swizzle<CHUNKS>(key))) * 16 + 8 * (in16 & 1);
-    // (eight keys further the swizzle is the same)
-    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)at);
-    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 8 * CHUNKS * 16));
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-}
+struct ValueReader {
+    static constexpr int kPlaces = CHUNKS == 12 ? 1 : CHUNKS / 4;
+    lds_bytes at[kPlaces];
+    __device__ __forceinline__ ValueReader(lds_bytes tile, int lane) {
+        const int in16 = lane & 15, key = 4 * (lane >> 5) + (in16 >> 2), c = 2 * (lane >> 4 & 1) + (in16 >> 1 & 1);
+#pragma unroll
+        for (int i = 0; i < kPlaces; ++i)
+            at[i] = (lds_bytes)(uintptr_t)(unsigned)opaque(
+                (int)(unsigned)(uintptr_t)(tile + (key * CHUNKS + ((4 * i + c) ^ v_swizzle<CHUNKS>(key))) * 16 + 8 * (in16 & 1)));
+    }
+    __device__ __forceinline__ v8s read(int offset, int key0, int block) const {
+        // (key0 a multiple of 8: the swizzle is the same)
+        lds_bytes const p = (CHUNKS == 12 ? at[0] + 64 * block : at[CHUNKS == 12 ? 0 : block]) + offset + key0 * CHUNKS * 16;
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p);
+        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + 8 * CHUNKS * 16));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
 
 // The key of register r of a block of S^T, less the block's first.
 __device__ __forceinline__ constexpr int key_of(int r) { return (r & 3) + 8 * (r >> 2); }   // + 4 (lane / 32)

@@ -52,8 +52,12 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows(AttentionArgs a) {
     const int head_bytes = 2 * a.head_dim;
     const T* const k = (const T*)a.k + s.k0 * a.k_token + kv * a.k_head;
     const T* const v = (const T*)a.v + s.k0 * a.v_token + kv * a.v_head;
-    const int k_stride = (int)(2 * a.k_token), v_stride = (int)(2 * a.v_token);
-    const unsigned base = (unsigned)(uintptr_t)(lds_bytes)(lds) + wave * STAGES * kStage;
+    lds_bytes const own = (lds_bytes)lds + wave * STAGES * kStage;
+    const unsigned base = (unsigned)(uintptr_t)own;
+    const TileLoader<CHUNKS, kKeys, 64, false> k_load((int)(2 * a.k_token), head_bytes, lane);
+    const TileLoader<CHUNKS, kKeys, 64, true> v_load((int)(2 * a.v_token), head_bytes, lane);
+    const KeyReader<CHUNKS, STEPS> k_read(own, lane);
+    const ValueReader<CHUNKS> v_read(own, lane);
 
     for (int row0 = 0; row0 < rows; row0 += kRows) {
         const int r = min(row0 + (lane & 31), rows - 1);
@@ -68,8 +72,8 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows(AttentionArgs a) {
         auto ask = [&](int t, int to) {
             const int left = s.m - t * kKeys;
             const unsigned at = base + to * kStage;
-            load_tile<CHUNKS, kKeys, 64, false>(k + (long)t * kKeys * a.k_token, at, k_stride, left, head_bytes, lane);
-            load_tile<CHUNKS, kKeys, 64, true>(v + (long)t * kKeys * a.v_token, at + kTile, v_stride, left, head_bytes, lane);
+            k_load.ask(k + (long)t * kKeys * a.k_token, at, left, lane);
+            v_load.ask(v + (long)t * kKeys * a.v_token, at + kTile, left, lane);
         };
         if (t0 + wave < t1) ask(t0 + wave, 0);
         v8s q[STEPS];
@@ -95,10 +99,10 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows(AttentionArgs a) {
             } else {
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             }
-            lds_bytes const tile = (lds_bytes)lds + (wave * STAGES + stage) * kStage;
+            const int at = stage * kStage;
             v16f sc = {};
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) sc = mfma<TYPE>(read_k<CHUNKS>(tile, 0, i, lane), q[i], sc);
+            for (int i = 0; i < STEPS; ++i) sc = mfma<TYPE>(k_read.read(at, 0, i), q[i], sc);
             const int first = t * kKeys + 4 * half;
             float top = -kInf;
 #pragma unroll
@@ -127,7 +131,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows(AttentionArgs a) {
                 const v4i pp = {(int)p[4 * i], (int)p[4 * i + 1], (int)p[4 * i + 2], (int)p[4 * i + 3]};
 #pragma unroll
                 for (int c = 0; c < BLOCKS; ++c)
-                    o[c] = mfma<TYPE>(read_v<CHUNKS>(tile + kTile, 16 * i, c, lane), __builtin_bit_cast(v8s, pp), o[c]);
+                    o[c] = mfma<TYPE>(v_read.read(at + kTile, 16 * i, c), __builtin_bit_cast(v8s, pp), o[c]);
             }
             if (STAGES == 2) {
                 stage ^= 1;
