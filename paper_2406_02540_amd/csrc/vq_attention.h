@@ -50,6 +50,34 @@ __device__ __forceinline__ int split_begin(const AttentionArgs& a, int tiles, in
     return (int)((unsigned)tiles * (unsigned)split >> a.split_shift);
 }
 
+// Which item a workgroup takes (false: none), and which head of K and V.  Workgroup ids are dealt round-robin to the XCDs.  A head's
+// items go to one XCD (as far as the heads are a multiple of them), whose L2 then has its keys, or all heads of an item, whose
+// rows share memory lines of q and out where a head is no whole lines: with few keys those are the traffic, and a line that is written
+// from two XCDs is written in pieces.  2 x 16384 queries on 120 keys, 16 heads of 72: 48 us by heads, 42 together; 2048 sequences of 16
+// 97 and 88; 32 sequences of 1024 223 and 232; heads of 128 on 128 keys 43 and 45.
+constexpr int kAttentionXcds = 8;
+__device__ __forceinline__ bool place_of(const AttentionArgs& a, int& kv, int& item) {
+    if (a.heads_together) {
+        const unsigned j = blockIdx.x / kAttentionXcds, group = j / (unsigned)a.kv_heads;
+        kv = (int)(j - group * (unsigned)a.kv_heads);
+        item = (int)(group * kAttentionXcds + blockIdx.x % kAttentionXcds);
+    } else {
+        const unsigned j = blockIdx.x / (unsigned)a.kv_heads;
+        kv = (int)(blockIdx.x - j * (unsigned)a.kv_heads);
+        item = (int)j;
+    }
+    return item < a.items;
+}
+// The workgroups that place_of() has in mind, or 0: more than a launch takes.
+inline unsigned attention_grid(AttentionArgs& a, long tiles, int threads) {
+    const long items = tiles << a.split_shift, blocks = (items + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds * a.kv_heads;
+    if (items > 0x7FFFFF00 || blocks * threads >= 1l << 32) return 0;
+    a.tiles = (int)tiles;
+    a.items = (int)items;
+    a.heads_together = a.Tk / a.sequences <= 512 && a.head_dim % 64 != 0;
+    return (unsigned)(a.heads_together ? blocks : items * a.kv_heads);
+}
+
 // ---- tiles of K and V in LDS ---------------------------------------------------------------------------------
 // [key][CHUNKS of 16 bytes], the chunk of a key at chunk ^ swizzle(key), so that what the LDS serves at once lies in different banks:
 // K is read 16 bytes a lane, one chunk of 32 keys at a time (sixteen lanes are served together: keys 0-3, 12-15 and 20-27, or the

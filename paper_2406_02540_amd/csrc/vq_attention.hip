@@ -44,9 +44,9 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows(AttentionArgs a) {
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int half = lane >> 5;
-    const int kv = (int)(blockIdx.x % (unsigned)a.kv_heads);
-    const unsigned item = blockIdx.x / (unsigned)a.kv_heads;
-    const int split = (int)item & ((1 << a.split_shift) - 1), b = (int)(item >> a.split_shift);
+    int kv, item;
+    if (!place_of(a, kv, item)) return;
+    const int split = item & ((1 << a.split_shift) - 1), b = item >> a.split_shift;
     const Span s = span_of(a, b);
     const int rows = s.n * a.group;
     const int head_bytes = 2 * a.head_dim;
@@ -229,14 +229,14 @@ __global__ __launch_bounds__(256) void attention_join(AttentionArgs a) {
 }
 
 template <class TYPE, int WAVES, int STAGES>
-hipError_t launch_rows_as(const AttentionArgs& a, hipStream_t stream) {
-    const long blocks = ((long)a.sequences << a.split_shift) * a.kv_heads;
-    if (blocks * 64 * WAVES >= 1l << 32) return hipErrorInvalidValue;
+hipError_t launch_rows_as(AttentionArgs a, hipStream_t stream) {
+    const unsigned blocks = attention_grid(a, a.sequences, 64 * WAVES);
+    if (!blocks) return hipErrorInvalidValue;
     void (*kernel)(AttentionArgs) = a.head_dim <= 64   ? attention_rows<TYPE, 8, 4, WAVES, STAGES>
                                     : a.head_dim <= 80 ? attention_rows<TYPE, 12, 5, WAVES, STAGES>
                                     : a.head_dim <= 96 ? attention_rows<TYPE, 12, 6, WAVES, STAGES>
                                                        : attention_rows<TYPE, 16, 8, WAVES, STAGES>;
-    return enqueue(kernel, dim3((unsigned)blocks), dim3(64 * WAVES), stream, a);
+    return enqueue(kernel, dim3(blocks), dim3(64 * WAVES), stream, a);
 }
 // A wavefront alone, one tile of keys at a time, where the average sequence has a few tiles and there are sequences enough.
 template <class TYPE>

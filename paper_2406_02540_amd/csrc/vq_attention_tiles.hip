@@ -35,12 +35,12 @@ __global__ __launch_bounds__(64 * kWaves, CHUNKS == 16 ? 2 : 3) void attention_t
     typedef typename TYPE::T T;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int kv = (int)(blockIdx.x % (unsigned)a.kv_heads);
-    const unsigned rest = blockIdx.x / (unsigned)a.kv_heads;
-    const int split = (int)rest & ((1 << a.split_shift) - 1);
+    int kv, item;
+    if (!place_of(a, kv, item)) return;
+    const int split = item & ((1 << a.split_shift) - 1);
     int tile;
     // (the last tiles of a sequence see the most keys: they go first)
-    const int b = find_sequence(a, a.items - 1 - (int)(rest >> a.split_shift), tile);
+    const int b = find_sequence(a, a.tiles - 1 - (item >> a.split_shift), tile);
     const Span s = span_of(a, b);
     const int rows = s.n * a.group, row0 = tile * kTileRows;
     if (tile < 0 || row0 >= rows) return;
@@ -217,14 +217,13 @@ __global__ __launch_bounds__(64 * kWaves, CHUNKS == 16 ? 2 : 3) void attention_t
 
 template <class TYPE>
 hipError_t launch(AttentionArgs a, hipStream_t stream) {
-    const long items = attention_items(a.sequences, a.Tq, a.group), blocks = (items << a.split_shift) * a.kv_heads;
-    a.items = (int)items;
-    if (items > 0x7FFFFFFF || blocks * 64 * kWaves >= 1l << 32) return hipErrorInvalidValue;
+    const unsigned blocks = attention_grid(a, attention_items(a.sequences, a.Tq, a.group), 64 * kWaves);
+    if (!blocks) return hipErrorInvalidValue;
     void (*kernel)(AttentionArgs) = a.head_dim <= 64   ? attention_tiles<TYPE, 8, 4>
                                     : a.head_dim <= 80 ? attention_tiles<TYPE, 12, 5>
                                     : a.head_dim <= 96 ? attention_tiles<TYPE, 12, 6>
                                                        : attention_tiles<TYPE, 16, 8>;
-    return enqueue(kernel, dim3((unsigned)blocks), dim3(64 * kWaves), stream, a);
+    return enqueue(kernel, dim3(blocks), dim3(64 * kWaves), stream, a);
 }
 
 }  // namespace

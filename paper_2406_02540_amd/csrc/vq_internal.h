@@ -131,7 +131,9 @@ struct AttentionArgs {
     float* part_o;            // [splits][Tq * heads][head_dim] and [splits][Tq * heads][2]: sums, maxima and weights
     float* part_ml;
     int split_shift;          // 2^split_shift workgroups divide the keys of a tile
-    int items;                // attention_items(): tiles of query rows, the launch's
+    int tiles;                // the launch's: tiles of query rows (attention_items()) or sequences,
+    int items;                // these for every part of their keys,
+    int heads_together;       // and whether an item's heads of K and V go to one XCD, or a head's items
 };
 // The logarithm of the workgroups that divide the keys of a tile, from the sizes alone.  Tq * heads < 2^31.
 int attention_split_shift(int sequences, int Tq, int Tk, int heads, int kv_heads);
