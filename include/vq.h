@@ -367,7 +367,7 @@ size_t vq_linear_mx4_workspace_bytes(int M, int N, int K);
  *
  * vq_attention: out = softmax(softmax_scale * q k^T) v over packed sequences.
  *     q, out     [Tq, heads, head_dim]; k, v [Tk, kv_heads, head_dim]; heads % kv_heads == 0, head h
- *                reads head h / (heads / kv_heads) of k and v; Tq * heads < 2^31
+ *                reads head h / (heads / kv_heads) of k and v; Tq * heads and Tk at most 2^31 - 256
  *     cu_q, cu_k int32 [sequences + 1], ascending: sequence b has the query rows cu_q[b] ..
  *                cu_q[b+1] - 1 and the key rows cu_k[b] .. cu_k[b+1] - 1; the numbers may differ
  *                (cross attention, new tokens behind earlier ones) and may be 0
@@ -376,10 +376,10 @@ size_t vq_linear_mx4_workspace_bytes(int M, int N, int K);
  *     strides    host, eight of them: token and head of q, k, v, out
  *   Query rows in front of the first sequence or behind the last are left as they were.  Scores, softmax and sums
  *   are fp32; the weights exp(score - max) are rounded to dtype for the product with v (they
- *   multiply values of that type), their sum is that of the fp32 ones.  Not checked on the
+ *   multiply values of that type), their sum is that of the rounded ones (72 and 80 channels) or of the fp32 ones.  Not checked on the
  *   device: k, v of a sequence finite (a value that is not reaches all of that sequence's
  *   rows); cu_q, cu_k ascending and within Tq, Tk (violations give unspecified values in out, never a fault).
- *   head_dim % 8 == 0, at most VQ_MAX_HEAD_DIM.  The workspace (vq_attention_workspace_bytes, which
+ *   head_dim % 8 == 0, at most VQ_MAX_HEAD_DIM; softmax_scale within [1e-30, 1e30].  The workspace (vq_attention_workspace_bytes, which
  *   may be 0; 16-byte aligned) holds partial results where keys are divided among workgroups;
  *   two calls that may overlap in time need one each.
  */

@@ -240,6 +240,7 @@ bool strides_ok(const int64_t* s, int tokens, int heads, int head_dim, bool writ
     return true;
 }
 constexpr int64_t kMaxKeyStride = 1 << 23;   // a tile's offsets are 32-bit
+constexpr int kMaxRows = 0x7FFFFF00;         // rows and keys of a last tile fit an int
 
 }  // namespace
 
@@ -526,7 +527,9 @@ int vq_linear_mx4(const void* x, const float* chan_mul, const uint8_t* wq, const
     int num_cus = 0;
     const int arch = check_arch(&num_cus);
     if (arch != VQ_OK) return arch;
-    if (vq::small_mx4_layer(M, N, K))
+    // (as in enqueue_layer: in two launches y may be where x or its factors were)
+    const Range out{y, 2 * (size_t)M * N};
+    if (vq::small_mx4_layer(M, N, K) && !out.meets({x, 2 * (size_t)M * K}) && !out.meets({chan_mul, 4 * (size_t)K}))
         return launch_status(vq::launch_mx4_layer_small({nullptr, nullptr, wq, w_scale, bias, y, M, N, K, x, chan_mul}, dtype, (hipStream_t)hip_stream));
     v = launch_status(vq::launch_mx4_quantize(x, dtype, chan_mul, xq, x_scale, M, K, (hipStream_t)hip_stream));
     if (v != VQ_OK) return v;
@@ -593,7 +596,7 @@ size_t vq_attention_workspace_bytes(int sequences, int Tq, int Tk, int heads, in
     if (sequences <= 0 || Tq <= 0 || Tk < 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0 || head_dim <= 0 ||
         head_dim % 8 != 0 || head_dim > VQ_MAX_HEAD_DIM)
         return 0;
-    if ((int64_t)Tq * heads > 0x7FFFFFFF) return 0;
+    if ((int64_t)Tq * heads > kMaxRows || Tk > kMaxRows) return 0;
     const size_t parts = (size_t)1 << vq::attention_split_shift(sequences, Tq, Tk, heads, kv_heads);
     return parts == 1 ? 0 : parts * (size_t)Tq * (size_t)heads * (size_t)(head_dim + 2) * sizeof(float);
 }
@@ -603,8 +606,8 @@ int vq_attention(const void* q, const void* k, const void* v, void* out, int dty
                  float softmax_scale, int causal, void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
     if (sequences < 0 || Tq < 0 || Tk < 0 || heads <= 0 || kv_heads <= 0 || heads > 1 << 16 || heads % kv_heads != 0 ||
-        (int64_t)Tq * heads > 0x7FFFFFFF || head_dim <= 0 || head_dim % 8 != 0 || head_dim > VQ_MAX_HEAD_DIM || (causal != 0 && causal != 1) ||
-        !std::isfinite(softmax_scale) || !(softmax_scale > 0.0f))
+        (int64_t)Tq * heads > kMaxRows || Tk > kMaxRows || head_dim <= 0 || head_dim % 8 != 0 || head_dim > VQ_MAX_HEAD_DIM || (causal != 0 && causal != 1) ||
+        !(softmax_scale >= 1e-30f && softmax_scale <= 1e30f))
         return VQ_ERR_SHAPE;
     if (sequences == 0 || Tq == 0) return VQ_OK;
     if (!q || !out || !cu_q || !cu_k || !strides || (Tk > 0 && (!k || !v))) return VQ_ERR_NULL;

@@ -42,8 +42,9 @@ __global__ __launch_bounds__(64 * kWaves, CHUNKS == 16 ? 2 : 3) void attention_t
     // (the last tiles of a sequence see the most keys: they go first)
     const int b = find_sequence(a, a.tiles - 1 - (item >> a.split_shift), tile);
     const Span s = span_of(a, b);
-    const int rows = s.n * a.group, row0 = tile * kTileRows;
-    if (tile < 0 || row0 >= rows) return;
+    const int rows = s.n * a.group;
+    if (tile < 0 || (unsigned)tile * kTileRows >= (unsigned)rows) return;
+    const int row0 = tile * kTileRows;
     const int head_bytes = 2 * a.head_dim;
     const T* const k = (const T*)a.k + s.k0 * a.k_token + kv * a.k_head;
     const T* const v = (const T*)a.v + s.k0 * a.v_token + kv * a.v_head;

@@ -332,6 +332,7 @@ Mx4Choice choose_mx4_gemm(int M, int N, int K, int num_cus) {
     float least = 0;
     auto consider = [&](int t, int c, bool divide, int resident, float start, float each) {
         const long tiles = ((long)M + t - 1) / t * (((long)N + c - 1) / c), slots = (long)resident * num_cus;
+        if (divide && tiles * 512 >= 1l << 32) return;       // (HIP takes less than 2^32 threads; the others are persistent)
         const float cost = start + (float)((tiles + slots - 1) / slots) * each;
         if (best.tile_t && cost >= least) return;
         best = {t, c, divide};
@@ -365,3 +366,10 @@ hipError_t launch_mx4_gemm(const Mx4GemmArgs& g, int dtype, int num_cus, hipStre
 }
 
 }  // namespace vq
+
+extern "C" void vq_internal_mx4_choice(int M, int N, int K, int num_cus, int choice[3]) {
+    const vq::Mx4Choice c = vq::choose_mx4_gemm(M, N, K, num_cus);
+    choice[0] = c.tile_t;
+    choice[1] = c.tile_c;
+    choice[2] = c.divide_k;
+}

@@ -92,6 +92,38 @@ def test_long_prompt():
     _run([3001], [3001], 2, 2, 72, F16, False)
 
 
+def test_no_keys_at_all():
+    for n in (2, 300):
+        q = torch.randn(n, 4, 72, device="cuda").to(F16)
+        kv = torch.empty(0, 2, 72, dtype=F16, device="cuda")
+        out = torch.full_like(q, 3.0)
+        cu = torch.tensor([0, n - 1, n - 1], dtype=torch.int32, device="cuda")
+        vq.vq_attention(q, kv, kv, cu, torch.zeros(3, dtype=torch.int32, device="cuda"), out=out)
+        assert (out[:n - 1] == 0).all() and (out[n - 1] == 3).all()
+
+
+@pytest.mark.parametrize("heads,D", [(16, 72), (5, 80), (3, 88)])
+def test_few_keys_for_many_queries(heads, D):
+    # all heads of a tile on one XCD, numbers of tiles that are no multiple of the XCDs
+    _run([700, 0, 1300, 5], [120, 7, 64, 1], heads, heads, D, F16, False, before=2, behind=3)
+    _run([1000], [63], heads, 1, D, BF16, True)
+
+
+def test_scores_far_below_the_first_tile_s():
+    # the first tile's scores are large, the others' far below (and the other way round): the reference stays with the largest
+    D, m = 72, 700
+    g = torch.Generator(device="cuda").manual_seed(9)
+    for n in (1, 200):
+        q = torch.randn(n, 1, D, generator=g, device="cuda").to(F16)
+        for lo, hi in ((0, 64), (640, 700), (100, 101)):
+            k = torch.randn(m, 1, D, generator=g, device="cuda") * 0.3
+            k[lo:hi] += 20 * q[:1].float()
+            k = k.to(F16)
+            v = torch.randn(m, 1, D, generator=g, device="cuda").to(F16)
+            want, off = ou.attention(q, k, v, [n], [m], 0.3, False)
+            ou.check(vq.vq_attention(q, k, v, ou.offsets([n]).cuda(), ou.offsets([m]).cuda(), softmax_scale=0.3), want, off)
+
+
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("n", [1, 300])
 def test_large_scores(causal, n):

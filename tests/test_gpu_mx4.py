@@ -91,7 +91,35 @@ def test_scales_behind_the_last_block_are_not_looked_at():
 
 SIZES = [(1, 1, 32), (1, 16, 64), (1, 3456, 1152), (2, 130, 4096), (15, 17, 96), (16, 32, 128), (17, 100, 160), (33, 65, 224),
          (64, 64, 512), (65, 255, 1184), (127, 513, 352), (240, 2304, 4096), (300, 1152, 1152), (257, 511, 1152), (1001, 2821, 1184),
-         (2048, 1152, 256), (1030, 4600, 320)]
+         (100, 4090, 640), (2048, 1152, 256), (1030, 4600, 320)]
+
+
+# the large tiles, several a workgroup: whole and half stages of K, one stage, rows and channels that end inside a tile
+LARGE = [(8200, 4616, 1152), (16384, 2304, 320), (33000, 1160, 128), (4100, 8192, 512), (9000, 1153, 640), (20000, 1152, 96)]
+
+
+@pytest.mark.parametrize("M,N,K", LARGE)
+def test_large_product(M, N, K):
+    g = torch.Generator(device="cuda").manual_seed(M)
+    xq = torch.randint(0, 256, (M, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    wq = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    xs, ws = (torch.randint(118, 128, (n, vq.MX4_SCALE_STRIDE(K)), generator=g, device="cuda", dtype=torch.uint8) for n in (M, N))
+    bias = torch.randn(N, generator=g, device="cuda").to(F16)
+    y = torch.full((M + 1, N), 7.0, dtype=F16, device="cuda")
+    got = vq.vq_gemm_mx4(xq, xs, wq, ws, bias, y=y[:M])
+    assert (y[M] == 7).all() and torch.equal(got, vq.vq_gemm_mx4(xq, xs, wq, ws, bias))
+    grid = torch.tensor(ou.E2M1 + tuple(-v for v in ou.E2M1), dtype=torch.float64, device="cuda")
+
+    def values(q, s):
+        v = grid[torch.stack((q & 15, q >> 4), -1).reshape(q.shape[0], -1).long()].reshape(q.shape[0], -1, 32)
+        return (v * torch.pow(2.0, s[:, :K // 32].double() - 127).unsqueeze(-1)).reshape(q.shape[0], K)
+
+    x, w = values(xq, xs), values(wq, ws)
+    for r in range(0, M, 8192):
+        part = x[r:r + 8192]
+        want, size = part @ w.t().contiguous() + bias.double(), part.abs() @ w.abs().t().contiguous() + bias.double().abs()
+        off = ou.HALF[F16] * want.abs() + ou.TINY[F16] + (32 + K // 32 + 2) * 2.0 ** -24 * size
+        assert ((got[r:r + 8192].double() - want).abs() <= off).all()
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
@@ -134,6 +162,29 @@ def test_layer_with_blocks_that_are_not_finite():
         wq, ws, _ = _quantized(_x(48, 256, F32, 1))
         y = vq.vq_linear_mx4(x.cuda(), None, wq, ws)
         assert y[1].isnan().all() and not y[0].isnan().any()
+
+
+@pytest.mark.parametrize("K", [32, 96, 128, 160, 288, 352, 1120, 2080])
+def test_nan_blocks_reach_their_row_only(K):
+    # in every kernel: the scale of one block of one token, and of one channel, NaN
+    for M, N in ((5, 40), (60, 100), (300, 2000), (4000, 1160), (9000, 1152)):
+        xq, ws = torch.full((M, K // 2), 0x22, dtype=torch.uint8, device="cuda"), torch.full((N, vq.MX4_SCALE_STRIDE(K)), 127, dtype=torch.uint8, device="cuda")
+        wq, xs = torch.full((N, K // 2), 0x22, dtype=torch.uint8, device="cuda"), torch.full((M, vq.MX4_SCALE_STRIDE(K)), 127, dtype=torch.uint8, device="cuda")
+        xs[M // 2, K // 32 - 1] = 255
+        ws[N - 1, 0] = 255
+        y = vq.vq_gemm_mx4(xq, xs, wq, ws)
+        assert y[M // 2].isnan().all() and y[:, N - 1].isnan().all()
+        assert y.isnan().sum().item() == M + N - 1
+        assert (y[:M // 2, :N - 1] == K).all() and (y[M // 2 + 1:, :N - 1] == K).all()
+
+
+def test_layer_into_its_own_activations():
+    # y where x was: the one launch would read what it has written
+    K = N = 256
+    x = _x(4, K, F16).cuda()
+    wq, ws, _ = _quantized(_x(N, K, F32, 1) * 0.1)
+    want = vq.vq_linear_mx4(x, None, wq, ws)
+    assert torch.equal(vq.vq_linear_mx4(x, None, wq, ws, y=x), want)
 
 
 def test_empty_sizes():

@@ -1,0 +1,53 @@
+"""The kernels of microscaled layers, rotary positions and attention: which one a product reaches, and that none spills registers."""
+import ctypes
+import os
+import re
+import subprocess
+
+import pytest
+
+from paper_2406_02540_amd import binding, build
+
+CUS = 256   # of an MI355X
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    if not os.path.exists(binding.LIB_PATH):
+        build.build(verbose=False)
+
+
+def choice(M, N, K):
+    """(tokens, channels, whether the wavefronts divide K) of the tile that a product takes."""
+    out = (ctypes.c_int * 3)()
+    binding.lib().vq_internal_mx4_choice(M, N, K, CUS, out)
+    return tuple(out)
+
+
+def test_every_tile_is_reached_by_the_gpu_tests():
+    pytest.importorskip("torch")
+    from test_gpu_mx4 import LARGE, SIZES
+    assert {choice(*s) for s in SIZES + LARGE} == {(256, 256, 0), (128, 128, 0), (64, 128, 0), (32, 32, 1), (48, 48, 1), (32, 64, 1)}
+
+
+def test_choice_of_large_and_ragged_rows():
+    assert choice(32768, 4608, 1152) == (256, 256, 0)
+    assert choice(32768, 4607, 1152)[0] < 256          # rows that are no whole pieces: not the largest tile
+    for M, N in ((700_000_000, 8), (1, 700_000_000), (1_000_000_000, 32)):
+        t, c, divide = choice(M, N, 32)
+        assert not divide or -(-M // t) * -(-N // c) * 512 < 2 ** 32
+
+
+@pytest.mark.parametrize("source", ["vq_mx4_quantize.hip", "vq_mx4_gemm.hip", "vq_mx4_gemm_split.hip", "vq_rotary.hip", "vq_attention.hip",
+                                    "vq_attention_tiles.hip"])
+def test_kernels_do_not_spill(source):
+    if not os.path.exists(build.hipcc()):
+        pytest.skip("no hipcc")
+    out = subprocess.run([build.hipcc(), *build.HIPCC_FLAGS, "-I", os.path.join(build.ROOT, "include"), "-I", build.CSRC,
+                          "--cuda-device-only", "-c", os.path.join(build.CSRC, source), "-o", os.devnull,
+                          "-Rpass-analysis=kernel-resource-usage"], capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0, out.stderr[-2000:]
+    names = re.findall(r"Function Name: (\S+)", out.stderr)
+    scratch = [int(b) for b in re.findall(r"ScratchSize \[bytes/lane\]: (\d+)", out.stderr)]
+    assert len(names) == len(scratch) > 0
+    assert {n: b for n, b in zip(names, scratch) if b} == {}

@@ -99,7 +99,7 @@ def test_attention_refusals(lib):
 
     assert [a(t=2), a(t=7)] == [TYPE] * 2
     assert [a(B=-1), a(Tq=-1), a(Tk=-1), a(H=0), a(G=0), a(G=3), a(D=0), a(D=100), a(D=136), a(causal=2), a(scale=0.0), a(scale=-1.0),
-            a(scale=math.inf), a(scale=math.nan), a(H=1 << 17, G=1)] == [SHAPE] * 15
+            a(scale=math.inf), a(scale=math.nan), a(H=1 << 17, G=1), a(scale=1e-31), a(scale=1e31), a(Tq=1 << 28), a(Tk=2**31 - 1)] == [SHAPE] * 19
     assert [a(q=None), a(k=None), a(v=None), a(o=None), a(cq=None), a(ck=None), a(s=None)] == [NULL] * 7
     assert [a(q=A + 2), a(k=A + 8), a(v=A + 8), a(o=A + 4), a(cq=A + 2), a(ck=A + 1)] == [ALIGN] * 6
     assert [a(s=(1020,) + dense[1:]), a(s=dense[:2] + (-8,) + dense[3:]), a(s=dense[:6] + (0, 128)), a(s=dense[:6] + (1024, 64)),
