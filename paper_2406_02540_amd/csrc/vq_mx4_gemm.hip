@@ -40,6 +40,7 @@ struct Shape {
 struct TileArgsMx {
     Mx4GemmArgs g;
     int tiles_t, tiles_c, tiles, tiles_per_xcd, slots;
+    bool whole_lines;        // rows of Y start on memory lines
 };
 
 // ROWS16: rows of Y are whole 16-byte pieces (N % 8 == 0, Y on 16 bytes): range-checked stores.  Otherwise 64-bit addresses.
@@ -161,20 +162,48 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void mx4_gemm(TileArgsMx a) {
         if (ROWS16) {
             const auto ry = __builtin_amdgcn_make_buffer_rsrc(y, 0, (int)(2 * ((unsigned)(rows - 1) * (unsigned)N + (unsigned)cols)), (int)kRsrcFlags);
             const lds_bytes bias = (lds_bytes)lds + S::kBias + bias_from * S::kBiasBytes;
+            // A lane has eight channels of its token in each of two neighbouring pairs of blocks, 64 bytes of a token's row a store.  Lanes
+            // eight tokens apart exchange one of the two, and a store is 128 bytes of eight tokens: past the caches where these are whole
+            // lines (32768 x 1152 -> 4608 123 us, 130 through them, 8192 x 1152 -> 1152 15.0 and 16.9; halves of lines past the caches 138),
+            // through them where rows start elsewhere and neighbouring stores share lines.
+            const bool low = r16 < 8;
 #pragma unroll
-            for (int c = 0; c < S::CC; c += 2) {
+            for (int c = 0; c < S::CC; c += 4) {
                 const int n = 16 * (S::CC * wc + c) + 8 * g;
-                const v4i b8 = *(__attribute__((address_space(3))) v4i*)(bias + 2 * n);
-                float b[8];
+                float b[2][8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) TYPE::unpack((unsigned)b8[e], b[2 * e], b[2 * e + 1]);
-                const int at = n < cols ? 2 * ((16 * S::TT * wt + r16) * N + n) : kNowhere;
+                for (int h = 0; h < 2; ++h) {
+                    const v4i b8 = *(__attribute__((address_space(3))) v4i*)(bias + 2 * (n + 32 * h));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) TYPE::unpack((unsigned)b8[e], b[h][2 * e], b[h][2 * e + 1]);
+                }
+                const int to = n + (low ? 0 : 32);
+                const int at = to < cols ? 2 * ((16 * S::TT * wt + (r16 & 7)) * N + to) : kNowhere;
 #pragma unroll
                 for (int t = 0; t < S::TT; ++t) {
-                    const v4f lo = acc[t][c], hi = acc[t][c + 1];
-                    const v4u out = {TYPE::pack(lo[0] + b[0], lo[1] + b[1]), TYPE::pack(lo[2] + b[2], lo[3] + b[3]),
-                                     TYPE::pack(hi[0] + b[4], hi[1] + b[5]), TYPE::pack(hi[2] + b[6], hi[3] + b[7])};
-                    __builtin_amdgcn_raw_buffer_store_b128(out, ry, n < cols ? at + 32 * t * N : kNowhere, 0, 0);
+                    v4u piece[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const v4f lo = acc[t][c + 2 * h], hi = acc[t][c + 2 * h + 1];
+                        piece[h] = v4u{TYPE::pack(lo[0] + b[h][0], lo[1] + b[h][1]), TYPE::pack(lo[2] + b[h][2], lo[3] + b[h][3]),
+                                       TYPE::pack(hi[0] + b[h][4], hi[1] + b[h][5]), TYPE::pack(hi[2] + b[h][6], hi[3] + b[h][7])};
+                    }
+                    v4u first, second;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned given = low ? piece[1][e] : piece[0][e];
+                        const unsigned taken = (unsigned)__builtin_amdgcn_mov_dpp((int)given, 0x128, 0xF, 0xF, true);    // row_ror:8
+                        first[e] = low ? piece[0][e] : taken;
+                        second[e] = low ? taken : piece[1][e];
+                    }
+                    const int at_first = to < cols ? at + 32 * t * N : kNowhere, at_second = to < cols ? at + 32 * t * N + 16 * N : kNowhere;
+                    if (a.whole_lines) {
+                        __builtin_amdgcn_raw_buffer_store_b128(first, ry, at_first, 0, 2 /* nontemporal */);
+                        __builtin_amdgcn_raw_buffer_store_b128(second, ry, at_second, 0, 2);
+                    } else {
+                        __builtin_amdgcn_raw_buffer_store_b128(first, ry, at_first, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b128(second, ry, at_second, 0, 0);
+                    }
                 }
             }
         } else {
@@ -301,7 +330,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void mx4_gemm(TileArgsMx a) {
 
 template <class S>
 hipError_t launch(const Mx4GemmArgs& g, int dtype, int num_cus, hipStream_t stream) {
-    TileArgsMx a{g, 0, 0, 0, 0, 0};
+    TileArgsMx a{g, 0, 0, 0, 0, 0, g.N % 64 == 0 && (uintptr_t)g.y % 128 == 0};
     if (g.M > 0x7FFFFF00 || g.N > 0x7FFFFF00) return hipErrorInvalidValue;     // (rows and channels of a last tile fit an int)
     a.tiles_t = (g.M + S::kTok - 1) / S::kTok;
     a.tiles_c = (g.N + S::kCh - 1) / S::kCh;
