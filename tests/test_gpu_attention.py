@@ -109,6 +109,14 @@ def test_few_keys_for_many_queries(heads, D):
     _run([1000], [63], heads, 1, D, BF16, True)
 
 
+@pytest.mark.parametrize("H,G,D", [(16, 16, 72), (16, 16, 64), (32, 8, 128), (16, 16, 88), (20, 20, 80)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_few_keys_kept(H, G, D, dtype):
+    # query rows for more than two workgroups a CU: those that keep the keys (and go through more than 128 in turns)
+    _run([6000, 1, 0, 2999, 40], [128, 0, 9, 75, 33], H, G, D, dtype, False, before=1, behind=2)
+    _run([3000, 4500, 7, 1500], [300, 1, 64, 129], H, G, D, dtype, False)
+
+
 def test_scores_far_below_the_first_tile_s():
     # the first tile's scores are large, the others' far below (and the other way round): the reference stays with the largest
     D, m = 72, 700
