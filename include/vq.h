@@ -355,7 +355,7 @@ size_t vq_linear_mx4_workspace_bytes(int M, int N, int K);
  *     positions  int32 [T], any value (the negative of a position undoes it)
  *     inv_freq   fp32 [rot_dim/2]
  *     strides    host, eight of them: token and head of q, q_out, k, k_out
- *   head_dim % 8 == 0, at most VQ_MAX_HEAD_DIM; rot_dim % 8 == 0, 0 < rot_dim <= head_dim.  In place
+ *   head_dim % 8 == 0, at most VQ_MAX_HEAD_DIM; rot_dim even, 0 < rot_dim <= head_dim.  In place
  *   (q_out == q with the same strides) is allowed; no other overlap is.
  *
  * vq_rotary_frequencies: host-only, fills inv_freq [rot_dim/2] (HOST memory) and the amplitude for it.

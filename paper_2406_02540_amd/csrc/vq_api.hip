@@ -541,7 +541,7 @@ int vq_rotary(const void* q, void* q_out, const void* k, void* k_out, int dtype,
               int rot_dim, const int64_t* strides, void* hip_stream) {
     if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
     if (T < 0 || q_heads <= 0 || k_heads < 0 || q_heads > 1 << 16 || k_heads > 1 << 16 || head_dim <= 0 || head_dim % 8 != 0 ||
-        head_dim > VQ_MAX_HEAD_DIM || rot_dim <= 0 || rot_dim % 8 != 0 || rot_dim > head_dim ||
+        head_dim > VQ_MAX_HEAD_DIM || rot_dim <= 0 || rot_dim % 2 != 0 || rot_dim > head_dim ||
         (interleaved != 0 && interleaved != 1) || !std::isfinite(amplitude))
         return VQ_ERR_SHAPE;
     if (T == 0) return VQ_OK;

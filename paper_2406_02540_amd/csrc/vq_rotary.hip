@@ -18,10 +18,11 @@ __device__ __forceinline__ void rotation(int position, float freq, float amplitu
     s *= amplitude;
 }
 
-// A thread takes four neighbouring pairs of a token, computes their angles once and turns them in every `lanes_h`-th head, q's and
-// k's one after the other (threads behind the pairs copy eight channels that are not turned).  Neighbouring threads take
-// neighbouring pairs, then heads: a wavefront's accesses cover whole rows of a token.
-template <class TYPE, bool INTERLEAVED>
+// A thread takes PAIRS neighbouring pairs of a token, computes their angles once and turns them in every `lanes_h`-th head, q's and
+// k's one after the other (threads behind the pairs copy as many channels that are not turned).  Neighbouring threads take
+// neighbouring pairs, then heads: a wavefront's accesses cover whole rows of a token.  Four pairs where the heads' turned part
+// divides by them, else two, else one: the second halves start at rot_dim / 2, and with them the accesses' alignment.
+template <class TYPE, bool INTERLEAVED, int PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a) {
     const int pieces = a.copied_from + a.copied;       // per head: four pairs, or eight channels to copy
     const int heads = a.q_heads + a.k_heads;
@@ -41,40 +42,47 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a) {
             h = (int)(rest - (long)token * a.lanes_h);
         }
         typedef typename TYPE::T T;
+        typedef int Piece __attribute__((ext_vector_type(PAIRS)));          // a piece's channels, neighbours in pairs
+        typedef short Half __attribute__((ext_vector_type(PAIRS)));         // those of one half
+        typedef short Both __attribute__((ext_vector_type(2 * PAIRS)));
+        typedef float Angles __attribute__((ext_vector_type(PAIRS)));
         const T* const q = (const T*)a.q + token * a.q_token;
         const T* const k = (const T*)a.k + token * a.k_token;
         T* const qo = (T*)a.q_out + token * a.qo_token;
         T* const ko = (T*)a.k_out + token * a.ko_token;
         if (piece >= a.copied_from) {
-            const int at = a.rot_dim + 8 * (piece - a.copied_from);
+            const int at = a.rot_dim + 2 * PAIRS * (piece - a.copied_from);
             for (; h < heads; h += a.lanes_h) {
                 const bool is_q = h < a.q_heads;
                 const int hk = h - a.q_heads;
-                *(v4i*)((is_q ? qo + h * a.qo_head : ko + hk * a.ko_head) + at) =
-                    *(const v4i*)((is_q ? q + h * a.q_head : k + hk * a.k_head) + at);
+                *(Piece*)((is_q ? qo + h * a.qo_head : ko + hk * a.ko_head) + at) =
+                    *(const Piece*)((is_q ? q + h * a.q_head : k + hk * a.k_head) + at);
             }
             continue;
         }
         const int position = a.positions[token];
-        const v4f freq = *(const v4f*)(a.inv_freq + 4 * piece);
-        float c[4], s[4];
+        const Angles freq = *(const Angles*)(a.inv_freq + PAIRS * piece);
+        float c[PAIRS], s[PAIRS];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) rotation(position, freq[e], a.amplitude, c[e], s[e]);
+        for (int e = 0; e < PAIRS; ++e) rotation(position, freq[e], a.amplitude, c[e], s[e]);
         const int half = a.rot_dim / 2;
         // (kAtOnce heads' loads are on their way together: 32768 tokens, 16 + 16 heads of 72, halves 70 us with one, 65 so,
         // 4.3 and 4.7 TB/s; neighbouring pairs 51.6 and 49.3)
         for (; h < heads; h += kAtOnce * a.lanes_h) {
-            v4i in[kAtOnce];
+            Piece in[kAtOnce];
 #pragma unroll
             for (int u = 0; u < kAtOnce; ++u) {
                 const int hu = h + u * a.lanes_h;
                 if (hu >= heads) break;
                 const T* const from = hu < a.q_heads ? q + hu * a.q_head : k + (hu - a.q_heads) * a.k_head;
                 if (INTERLEAVED) {
-                    in[u] = *(const v4i*)(from + 8 * piece);
+                    in[u] = *(const Piece*)(from + 2 * PAIRS * piece);
                 } else {
-                    const v2i va = *(const v2i*)(from + 4 * piece), vb = *(const v2i*)(from + half + 4 * piece);
-                    in[u] = v4i{va[0], va[1], vb[0], vb[1]};
+                    const Half first = *(const Half*)(from + PAIRS * piece), second = *(const Half*)(from + half + PAIRS * piece);
+                    Both both;
+#pragma unroll
+                    for (int e = 0; e < PAIRS; ++e) both[e] = first[e], both[PAIRS + e] = second[e];
+                    in[u] = __builtin_bit_cast(Piece, both);
                 }
             }
 #pragma unroll
@@ -82,38 +90,51 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a) {
                 const int hu = h + u * a.lanes_h;
                 if (hu >= heads) break;
                 T* const out = hu < a.q_heads ? qo + hu * a.qo_head : ko + (hu - a.q_heads) * a.ko_head;
-                float x[4], y[4];
-                v4i o;
-                if (INTERLEAVED) {
+                float x[PAIRS], y[PAIRS];
+                Piece o;
+                if (INTERLEAVED || PAIRS == 1) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
+                    for (int e = 0; e < PAIRS; ++e) {
                         TYPE::unpack((unsigned)in[u][e], x[e], y[e]);
                         o[e] = (int)TYPE::pack(x[e] * c[e] - y[e] * s[e], y[e] * c[e] + x[e] * s[e]);
                     }
-                    *(v4i*)(out + 8 * piece) = o;
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int i0 = 2 * e, i1 = 2 * e + 1;
+                    for (int e = 0; e < PAIRS / 2; ++e) {
+                        const int i0 = 2 * e, i1 = 2 * e + 1, b = PAIRS / 2 + e;
                         TYPE::unpack((unsigned)in[u][e], x[i0], x[i1]);
-                        TYPE::unpack((unsigned)in[u][2 + e], y[i0], y[i1]);
+                        TYPE::unpack((unsigned)in[u][b], y[i0], y[i1]);
                         o[e] = (int)TYPE::pack(x[i0] * c[i0] - y[i0] * s[i0], x[i1] * c[i1] - y[i1] * s[i1]);
-                        o[2 + e] = (int)TYPE::pack(y[i0] * c[i0] + x[i0] * s[i0], y[i1] * c[i1] + x[i1] * s[i1]);
+                        o[b] = (int)TYPE::pack(y[i0] * c[i0] + x[i0] * s[i0], y[i1] * c[i1] + x[i1] * s[i1]);
                     }
-                    *(v2i*)(out + 4 * piece) = v2i{o[0], o[1]};
-                    *(v2i*)(out + half + 4 * piece) = v2i{o[2], o[3]};
+                }
+                if (INTERLEAVED) {
+                    *(Piece*)(out + 2 * PAIRS * piece) = o;
+                } else {
+                    const Both both = __builtin_bit_cast(Both, o);
+                    Half first, second;
+#pragma unroll
+                    for (int e = 0; e < PAIRS; ++e) first[e] = both[e], second[e] = both[PAIRS + e];
+                    *(Half*)(out + PAIRS * piece) = first;
+                    *(Half*)(out + half + PAIRS * piece) = second;
                 }
             }
         }
     }
 }
 
+template <class TYPE, bool INTERLEAVED>
+void (*kernel_of(int pairs))(RotaryArgs) {
+    return pairs == 4 ? rotary<TYPE, INTERLEAVED, 4> : pairs == 2 ? rotary<TYPE, INTERLEAVED, 2> : rotary<TYPE, INTERLEAVED, 1>;
+}
+
 }  // namespace
 
 hipError_t launch_rotary(RotaryArgs a, int dtype, int interleaved, hipStream_t stream) {
     const bool in_place = a.q == a.q_out && (a.k_heads == 0 || a.k == a.k_out);
-    a.copied_from = a.rot_dim / 8;
-    a.copied = in_place ? 0 : (a.head_dim - a.rot_dim) / 8;
+    const int pairs = a.rot_dim % 8 == 0 ? 4 : a.rot_dim % 4 == 0 ? 2 : 1;
+    a.copied_from = a.rot_dim / (2 * pairs);
+    a.copied = in_place ? 0 : (a.head_dim - a.rot_dim) / (2 * pairs);
     const int pieces = a.copied_from + a.copied, heads = a.q_heads + a.k_heads;
     // heads that a thread turns one after another: as many as leave the chip full
     int turns = 8;
@@ -122,8 +143,8 @@ hipError_t launch_rotary(RotaryArgs a, int dtype, int interleaved, hipStream_t s
     const long all = (long)a.T * a.lanes_h * pieces;
     long blocks = (all + kThreads - 1) / kThreads;
     if (blocks > 1 << 20) blocks = 1 << 20;
-    void (*kernel)(RotaryArgs) = dtype == VQ_F16 ? (interleaved ? rotary<F16, true> : rotary<F16, false>)
-                                                 : (interleaved ? rotary<BF16, true> : rotary<BF16, false>);
+    void (*kernel)(RotaryArgs) = dtype == VQ_F16 ? (interleaved ? kernel_of<F16, true>(pairs) : kernel_of<F16, false>(pairs))
+                                                 : (interleaved ? kernel_of<BF16, true>(pairs) : kernel_of<BF16, false>(pairs));
     return enqueue(kernel, dim3((unsigned)blocks), dim3(kThreads), stream, a);
 }
 

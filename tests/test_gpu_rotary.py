@@ -23,7 +23,8 @@ def _check(got, x, p, f, interleaved, amplitude, what):
 
 
 @pytest.mark.parametrize("T,H,G,D,R", [(1, 1, 1, 8, 8), (1, 32, 8, 128, 64), (7, 3, 1, 64, 64), (100, 16, 16, 72, 72),
-                                       (33, 5, 5, 80, 16), (513, 4, 2, 96, 40), (3000, 16, 16, 72, 72)])
+                                       (33, 5, 5, 80, 16), (513, 4, 2, 96, 40), (3000, 16, 16, 72, 72),
+                                       (300, 8, 2, 72, 36), (5, 2, 1, 72, 18), (1100, 32, 8, 128, 124), (9, 3, 3, 8, 2), (65, 4, 1, 64, 62)])
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("dtype", [F16, BF16])
 def test_slices(T, H, G, D, R, interleaved, dtype):

@@ -79,15 +79,15 @@ def test_rotary_refusals(lib):
         return lib.vq_rotary(P(q), P(qo), P(k), P(ko), t, P(p), P(f), F(amp), inter, T, hq, hk, D, R, _strides(*s) if s else None, None)
 
     assert [r(t=2), r(t=-1)] == [TYPE] * 2
-    assert [r(T=-1), r(hq=0), r(hk=-1), r(D=0), r(D=12), r(D=136), r(R=0), r(R=20), r(R=136), r(inter=2), r(amp=math.inf),
+    assert [r(T=-1), r(hq=0), r(hk=-1), r(D=0), r(D=12), r(D=136), r(R=0), r(R=21), r(R=136), r(inter=2), r(amp=math.inf),
             r(amp=math.nan), r(hq=1 << 17)] == [SHAPE] * 13
     assert [r(q=None), r(qo=None), r(k=None), r(ko=None), r(p=None), r(f=None), r(s=None)] == [NULL] * 7
     assert [r(q=A + 8), r(qo=A + 2), r(k=A + 4), r(ko=A + 8), r(p=A + 2), r(f=A + 4)] == [ALIGN] * 6
     # strides: whole 16 bytes, not negative; rows that are written lie apart
     assert [r(s=(1020,) + dense[1:]), r(s=(-8,) + dense[1:]), r(s=dense[:2] + (1024, 64) + dense[4:]), r(s=dense[:2] + (0, 128) + dense[4:]),
             r(qo=A, s=(1024, 128, 2048, 128) + dense[4:]), r(ko=3 * A, s=dense[:6] + (1024, 256))] == [SHAPE] * 6
-    assert [r(T=0, q=None), r(), r(s=(0, 0) + dense[2:]), r(hk=0, k=None, ko=None), r(qo=A, ko=3 * A), r(p=A + 4), r(T=1, s=dense[:2] + (0, 128) + dense[4:])] == \
-        [OK] + [ARCH] * 6
+    assert [r(T=0, q=None), r(), r(s=(0, 0) + dense[2:]), r(R=20), r(R=18), r(hk=0, k=None, ko=None), r(qo=A, ko=3 * A), r(p=A + 4), r(T=1, s=dense[:2] + (0, 128) + dense[4:])] == \
+        [OK] + [ARCH] * 8
 
 
 def test_attention_refusals(lib):
