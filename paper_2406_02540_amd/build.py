@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libvidiq.so")
 CEILINGS_PATH = os.path.join(PKG_DIR, "vq_ceilings")  # stand-alone program, see csrc/vq_ceilings.hip
 SOURCES = ["vq_api.hip", "vq_quantize.hip", "vq_fused.hip", "vq_fused_gelu.hip", "vq_gemm.hip", "vq_gemm_192.hip", "vq_gemm_192w4.hip", "vq_gemm_tiles.hip", "vq_gemm_split.hip",
            "vq_linear_small.hip", "vq_mx4_quantize.hip", "vq_mx4_gemm.hip", "vq_mx4_gemm_split.hip", "vq_rotary.hip", "vq_attention.hip",
-           "vq_attention_tiles.hip", "vq_attention_few.hip"]
+           "vq_attention_tiles.hip"]
 
 EXT_PATH = os.path.join(PKG_DIR, "_vq_torch.so")  # the torch side (csrc/vq_torch.cpp): host code only
 

@@ -38,20 +38,6 @@ __device__ __forceinline__ Span span_of(const AttentionArgs& a, int b) {
     return s;
 }
 
-// Tiles of 2^tile_shift rows of all sequences are numbered so that a sequence's first is floor(cu * group / rows of a tile) + b, at
-// least the tiles of the sequences in front of it (floor(x + y) - floor(x) + 1 >= ceil(y)): a sequence is found by bisection, and a
-// number that no tile has is a workgroup that ends at once.
-__device__ __forceinline__ int find_sequence(const AttentionArgs& a, int item, int tile_shift, int& tile) {
-    int lo = 0, hi = a.sequences - 1;
-    auto first = [&](int b) { return (int)((unsigned)(min(max(a.cu_q[b], 0), a.Tq) * a.group) >> tile_shift) + b; };
-    while (lo < hi) {
-        const int mid = lo + (hi - lo + 1) / 2;
-        if (first(mid) <= item) lo = mid;
-        else hi = mid - 1;
-    }
-    tile = item - first(lo);
-    return lo;
-}
 __device__ __forceinline__ int token_of(const AttentionArgs& a, int row) {
     return a.group_shift >= 0 ? row >> a.group_shift : (int)((unsigned)row / (unsigned)a.group);
 }
@@ -192,29 +178,6 @@ struct ValueReader {
 // The key of register r of a block of S^T, less the block's first.
 __device__ __forceinline__ constexpr int key_of(int r) { return (r & 3) + 8 * (r >> 2); }   // + 4 (lane / 32)
 
-__device__ __forceinline__ float other_half(float v) {
-    const unsigned u = __builtin_bit_cast(unsigned, v);
-    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    // (r[0]: the low half's value in both halves, r[1]: the high half's)
-    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
-}
-
-// The sum of a row's weights as one more channel, where heads of 72 and 80 channels leave a part of their last block free: V's first
-// column behind the head is ones.  It stays in LDS while keys come and go (TileLoader's KEEP); whatever keys behind a sequence's end
-// have there, their weights are zero.
-template <class TYPE, int CHUNKS>
-__device__ __forceinline__ void write_sum_column(lds_bytes tile, int keys, int first, int thread, int threads) {
-    for (int key = thread; key < keys; key += threads)
-        for (int c = first; c < CHUNKS; ++c)
-            *(__attribute__((address_space(3))) v4i*)(tile + (key * CHUNKS + c) * 16) = v4i{c == first ? (int)TYPE::pack(1.0f, 0.0f) : 0, 0, 0, 0};
-}
-// It is channel 72 or 80: 8 or 16 of the last block, in the wavefront's lower half.
-template <int BLOCKS>
-__device__ __forceinline__ float sum_of_column(const v16f* o, int head_dim, int half) {
-    const float sum = head_dim == 72 ? o[BLOCKS - 1][4] : o[BLOCKS - 1][8], other = other_half(sum);
-    return half ? other : sum;
-}
-
 // A wavefront's 32 rows of outputs, whose lanes' sums l and outputs o (relative to ref) are complete: normalised to `out`, or as they are
 // to the parts.  `row`: token (of all) and head of the lane's row.
 template <class TYPE, int BLOCKS>
@@ -247,6 +210,13 @@ __device__ __forceinline__ void write_rows(const AttentionArgs& a, const v16f* o
             }
         if (half == 0) *(v2f*)(a.part_ml + slot * 2) = v2f{l > 0 ? ref : -__builtin_inff(), l};
     }
+}
+
+__device__ __forceinline__ float other_half(float v) {
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    // (r[0]: the low half's value in both halves, r[1]: the high half's)
+    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
 }
 
 }  // namespace vq

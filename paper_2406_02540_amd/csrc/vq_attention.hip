@@ -252,17 +252,14 @@ int attention_split_shift(int sequences, int Tq, int Tk, int heads, int kv_heads
     const long keys = (long)Tk / sequences;
     const bool rows = attention_by_rows(sequences, Tq, group);
     // parts of at least 256 keys of the average sequence, and workgroups for eight turns of the chip, or one of tiles
-    const long items = (rows ? (long)sequences : attention_items(sequences, Tq, group, kTileShift)) * kv_heads;
+    const long items = (rows ? (long)sequences : attention_items(sequences, Tq, group)) * kv_heads;
     int shift = 0;
     while (shift < 6 && (items << shift) < (rows ? 2048 : 512) && keys >> (shift + 1) >= 256) ++shift;
     return shift;
 }
 
 hipError_t launch_attention(const AttentionArgs& a, int dtype, hipStream_t stream) {
-    // few keys, all of them seen, and tiles for more than two workgroups a CU
-    const bool few = !a.causal && a.split_shift == 0 && a.Tk / a.sequences <= 128 &&
-                     attention_items(a.sequences, a.Tq, a.group, kTileShift + 1) * a.kv_heads >= 512;
-    const hipError_t e = !attention_by_rows(a.sequences, a.Tq, a.group) ? (few ? launch_attention_few_keys : launch_attention_tiles)(a, dtype, stream)
+    const hipError_t e = !attention_by_rows(a.sequences, a.Tq, a.group) ? launch_attention_tiles(a, dtype, stream)
                          : dtype == VQ_F16                              ? launch_rows<F16>(a, stream)
                                                                         : launch_rows<BF16>(a, stream);
     if (e != hipSuccess || a.split_shift == 0) return e;

@@ -11,6 +11,21 @@ constexpr int kKeys = 64;
 constexpr float kInf = __builtin_inff();
 constexpr float kSlack = 8.0f;    // base 2: how far a score may exceed the reference before sums and outputs are rescaled
 
+// Tiles of all sequences are numbered so that a sequence's first is floor(cu * group / rows) + b, at least the tiles of the
+// sequences in front of it (floor(x + y) - floor(x) + 1 >= ceil(y)): a sequence is found by bisection, and a number that no tile has
+// is a workgroup that ends at once.
+__device__ __forceinline__ int find_sequence(const AttentionArgs& a, int item, int& tile) {
+    int lo = 0, hi = a.sequences - 1;
+    auto first = [&](int b) { return (int)((unsigned)(min(max(a.cu_q[b], 0), a.Tq) * a.group) / kTileRows) + b; };
+    while (lo < hi) {
+        const int mid = lo + (hi - lo + 1) / 2;
+        if (first(mid) <= item) lo = mid;
+        else hi = mid - 1;
+    }
+    tile = item - first(lo);
+    return lo;
+}
+
 template <class TYPE, int CHUNKS, int STEPS>
 __global__ __launch_bounds__(64 * kWaves, CHUNKS == 16 ? 2 : 3) void attention_tiles(AttentionArgs a) {
     constexpr int BLOCKS = CHUNKS / 4;
@@ -25,7 +40,7 @@ __global__ __launch_bounds__(64 * kWaves, CHUNKS == 16 ? 2 : 3) void attention_t
     const int split = item & ((1 << a.split_shift) - 1);
     int tile;
     // (the last tiles of a sequence see the most keys: they go first)
-    const int b = find_sequence(a, a.tiles - 1 - (item >> a.split_shift), kTileShift, tile);
+    const int b = find_sequence(a, a.tiles - 1 - (item >> a.split_shift), tile);
     const Span s = span_of(a, b);
     const int rows = s.n * a.group;
     if (tile < 0 || (unsigned)tile * kTileRows >= (unsigned)rows) return;
@@ -51,12 +66,21 @@ __global__ __launch_bounds__(64 * kWaves, CHUNKS == 16 ? 2 : 3) void attention_t
     auto ask_v = [&](int t, int to) {
         v_load.template ask<kSumColumn>(v + (long)t * kKeys * a.v_token, base + (2 + to) * kTile, s.m - t * kKeys, threadIdx.x);
     };
+    // The sum of a row's weights as one more channel: V's first column behind the head is ones, which stay in LDS (and whatever the keys
+    // behind a sequence's end have there, their weights are zero).
+    if (kSumColumn) {
+        const int first = a.head_dim / 8;
+        for (int i = threadIdx.x; i < 2 * kKeys * (CHUNKS - first); i += 64 * kWaves) {
+            const int key = i / (CHUNKS - first), c = first + i % (CHUNKS - first);
+            const int one = c == first ? (int)(TYPE::pack(1.0f, 0.0f)) : 0;
+            *(__attribute__((address_space(3))) v4i*)((lds_bytes)lds + 2 * kTile + (key * CHUNKS + c) * 16) = v4i{one, 0, 0, 0};
+        }
+    }
     if (t0 < t1) {
         ask_k(t0, 0);
         ask_v(t0, 0);
         if (t0 + 1 < t1) ask_k(t0 + 1, 1);
     }
-    if (kSumColumn) write_sum_column<TYPE, CHUNKS>((lds_bytes)lds + 2 * kTile, 2 * kKeys, a.head_dim / 8, threadIdx.x, 64 * kWaves);
     v8s q[STEPS];
     const T* const qr = (const T*)a.q + (s.q0 + token) * a.q_token + head * a.q_head;
 #pragma unroll
@@ -180,7 +204,12 @@ __global__ __launch_bounds__(64 * kWaves, CHUNKS == 16 ? 2 : 3) void attention_t
         for (; t + 1 < t1; ++t) step(t, std::true_type{});
         step(t, std::false_type{});
     }
-    l = kSumColumn ? sum_of_column<BLOCKS>(o, a.head_dim, half) : l + other_half(l);
+    if (kSumColumn) {       // (channel head_dim, 8 or 16 of the last block, in the lower half)
+        const float sum = a.head_dim == 72 ? o[BLOCKS - 1][4] : o[BLOCKS - 1][8], other = other_half(sum);
+        l = half ? other : sum;
+    } else {
+        l += other_half(l);
+    }
     // (the row's token and head once more: kept through the loop they would be registers that it does not have)
     const int last_lane = opaque(lane), row = min(row0 + 32 * wave + (last_lane & 31), rows - 1), its_token = token_of(a, row);
     write_rows<TYPE, BLOCKS>(a, o, ref, l, s.q0 + its_token, kv * a.group + row - its_token * a.group, split,
@@ -189,7 +218,7 @@ __global__ __launch_bounds__(64 * kWaves, CHUNKS == 16 ? 2 : 3) void attention_t
 
 template <class TYPE>
 hipError_t launch(AttentionArgs a, hipStream_t stream) {
-    const unsigned blocks = attention_grid(a, attention_items(a.sequences, a.Tq, a.group, kTileShift), 64 * kWaves);
+    const unsigned blocks = attention_grid(a, attention_items(a.sequences, a.Tq, a.group), 64 * kWaves);
     if (!blocks) return hipErrorInvalidValue;
     void (*kernel)(AttentionArgs) = a.head_dim <= 64   ? attention_tiles<TYPE, 8, 4>
                                     : a.head_dim <= 80 ? attention_tiles<TYPE, 12, 5>

@@ -131,20 +131,18 @@ struct AttentionArgs {
     float* part_o;            // [splits][Tq * heads][head_dim] and [splits][Tq * heads][2]: sums, maxima and weights
     float* part_ml;
     int split_shift;          // 2^split_shift workgroups divide the keys of a tile
-    int tile_shift;           // the launch's: the logarithm of a workgroup's query rows (few keys),
-    int tiles;                // tiles of query rows (attention_items()) or sequences,
+    int tiles;                // the launch's: tiles of query rows (attention_items()) or sequences,
     int items;                // these for every part of their keys,
     int heads_together;       // and whether an item's heads of K and V go to one XCD, or a head's items
 };
 // The logarithm of the workgroups that divide the keys of a tile, from the sizes alone.  Tq * heads < 2^31.
 int attention_split_shift(int sequences, int Tq, int Tk, int heads, int kv_heads);
 hipError_t launch_attention(const AttentionArgs& a, int dtype, hipStream_t stream);
-// Its kernels: few query rows a sequence (vq_attention.hip), tiles of kTileRows (vq_attention_tiles.hip), or more rows on few keys
-// (vq_attention_few.hip).  attention_items(): at most so many tiles of 2^shift rows for a head of K and V.
-constexpr int kTileShift = 7, kTileRows = 1 << kTileShift;
+// Its two kernels: few query rows a sequence (vq_attention.hip), or tiles of kTileRows (vq_attention_tiles.hip), at most
+// attention_items() of them for a head of K and V.
+constexpr int kTileRows = 128;
 inline bool attention_by_rows(int sequences, int Tq, int group) { return (long)Tq * group <= 32l * sequences; }
-inline long attention_items(int sequences, int Tq, int group, int shift) { return ((long)Tq * group >> shift) + sequences; }
-hipError_t launch_attention_few_keys(const AttentionArgs& a, int dtype, hipStream_t stream);
+inline long attention_items(int sequences, int Tq, int group) { return (long)Tq * group / kTileRows + sequences; }
 hipError_t launch_attention_tiles(const AttentionArgs& a, int dtype, hipStream_t stream);
 
 }  // namespace vq

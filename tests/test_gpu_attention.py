@@ -111,8 +111,7 @@ def test_few_keys_for_many_queries(heads, D):
 
 @pytest.mark.parametrize("H,G,D", [(16, 16, 72), (16, 16, 64), (32, 8, 128), (16, 16, 88), (20, 20, 80)])
 @pytest.mark.parametrize("dtype", [F16, BF16])
-def test_few_keys_kept(H, G, D, dtype):
-    # query rows for more than two workgroups a CU: those that keep the keys (and go through more than 128 in turns)
+def test_thousands_of_queries_to_few_keys(H, G, D, dtype):
     _run([6000, 1, 0, 2999, 40], [128, 0, 9, 75, 33], H, G, D, dtype, False, before=1, behind=2)
     _run([3000, 4500, 7, 1500], [300, 1, 64, 129], H, G, D, dtype, False)
 

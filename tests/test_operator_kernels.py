@@ -39,7 +39,7 @@ def test_choice_of_large_and_ragged_rows():
 
 
 @pytest.mark.parametrize("source", ["vq_mx4_quantize.hip", "vq_mx4_gemm.hip", "vq_mx4_gemm_split.hip", "vq_rotary.hip", "vq_attention.hip",
-                                    "vq_attention_tiles.hip", "vq_attention_few.hip"])
+                                    "vq_attention_tiles.hip"])
 def test_kernels_do_not_spill(source):
     if not os.path.exists(build.hipcc()):
         pytest.skip("no hipcc")
