@@ -53,8 +53,9 @@ __device__ __forceinline__ int split_begin(const AttentionArgs& a, int tiles, in
 // Which item a workgroup takes (false: none), and which head of K and V.  Workgroup ids are dealt round-robin to the XCDs.  A head's
 // items go to one XCD (as far as the heads are a multiple of them), whose L2 then has its keys, or all heads of an item, whose
 // rows share memory lines of q and out where a head is no whole lines: with few keys those are the traffic, and a line that is written
-// from two XCDs is written in pieces.  2 x 16384 queries on 120 keys, 16 heads of 72: 48 us by heads, 42 together; 2048 sequences of 16
-// 97 and 88; 32 sequences of 1024 223 and 232; heads of 128 on 128 keys 43 and 45.
+// from two XCDs is written in pieces.  2 x 16384 queries on 120 keys, 16 heads of 72: 65.6 us by heads, 59.5 together (captured, inputs
+// that are not in the caches); 2048 sequences of 16 93.7 and 84; heads of 96 34.9 and 33.9.  With many keys they are better by heads: 32
+// sequences of 1024 223 and 232; so are heads of whole lines: of 128 on 128 keys 43 and 45 (both with inputs in the caches).
 constexpr int kAttentionXcds = 8;
 __device__ __forceinline__ bool place_of(const AttentionArgs& a, int& kv, int& item) {
     if (a.heads_together) {

@@ -141,6 +141,9 @@ hipError_t launch_attention(const AttentionArgs& a, int dtype, hipStream_t strea
 // Its two kernels: few query rows a sequence (vq_attention.hip), or tiles of kTileRows (vq_attention_tiles.hip), at most
 // attention_items() of them for a head of K and V.
 constexpr int kTileRows = 128;
+// Rows of the average sequence: up to 32, one MFMA block of them.  With all in tiles 16 single tokens over long keys take 230 us instead
+// of 170 and 2048 sequences of 16 239 instead of 84 (64 equal ones over 4096 keys 191 and 215); with up to 64 by rows 16 sequences of 64 rows over
+// 4096 keys 151 instead of 71 and 512 sequences of 64 91 instead of 75.
 inline bool attention_by_rows(int sequences, int Tq, int group) { return (long)Tq * group <= 32l * sequences; }
 inline long attention_items(int sequences, int Tq, int group) { return (long)Tq * group / kTileRows + sequences; }
 hipError_t launch_attention_tiles(const AttentionArgs& a, int dtype, hipStream_t stream);

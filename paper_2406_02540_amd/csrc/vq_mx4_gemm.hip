@@ -3,11 +3,17 @@
 // y[m,n] = sum over blocks of 2^(Ex + Ew) * (sum of 32 products of codes) + bias[n].  v_mfma_scale_f32_16x16x128_f8f6f4
 // multiplies 16 channels x 16 tokens x 4 blocks; lane l holds block l/16 of row l%16, 16 bytes as they lie in memory, and that
 // block's scale byte.  Channels are the rows of the product, so that a lane ends with four channels of a token, and the
-// channels are dealt to the rows of the weight tile so that its sums of two neighbouring MFMA blocks are eight channels in a row: a
-// store is 16 bytes a lane, 16 tokens x 64 bytes.
+// channels are dealt to the rows of the weight tile so that its sums of two neighbouring MFMA blocks are eight channels in a row; a
+// store, after an exchange between lanes, is 16 bytes a lane, 8 tokens x 128 bytes.
 //
-// K in stages of 256: a row is one cache line of codes (128 bytes) and two dwords of scales.  Both go from memory to LDS without
-// registers; the stage behind the one that is multiplied is on its way meanwhile, also from one tile of a workgroup to its next.
+// K in stages of 256: a row is one cache line of codes (128 bytes) and two dwords of scales.  The codes go from memory to LDS without
+// registers, the scales through a register of the thread that spreads them there; the stage behind the one that is multiplied is on
+// its way meanwhile, also from one tile of a workgroup to its next.
+//
+// Measured (captured, several hundred MB of inputs and outputs in turn, so that none is in the caches): 32768 x 1152 -> 4608 131 us (2.7
+// PFLOP/s; its 324 MB alone are 63 us at the 5.2 TB/s of a copy), 32768 x 4608 -> 1152 133, 8192 x 1152 -> 1152 16.6, 8192 x 8192 -> 8192
+// 277 (4.0 PFLOP/s).  Where K is long the matrix units are busy 42 % of the time at 2.07 GHz; where it is short a tile's outputs cost
+// as much as its products.
 #include "vq_internal.h"
 #include "vq_mx4_product.h"
 
@@ -164,7 +170,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void mx4_gemm(TileArgsMx a) {
             const lds_bytes bias = (lds_bytes)lds + S::kBias + bias_from * S::kBiasBytes;
             // A lane has eight channels of its token in each of two neighbouring pairs of blocks, 64 bytes of a token's row a store.  Lanes
             // eight tokens apart exchange one of the two, and a store is 128 bytes of eight tokens: past the caches where these are whole
-            // lines (32768 x 1152 -> 4608 123 us, 130 through them, 8192 x 1152 -> 1152 15.0 and 16.9; halves of lines past the caches 138),
+            // lines (32768 x 1152 -> 4608 131 us, 147 through them, 8192 x 1152 -> 1152 16.6 and 20.3; halves of lines past the caches are slower than either),
             // through them where rows start elsewhere and neighbouring stores share lines.
             const bool low = r16 < 8;
 #pragma unroll

@@ -1,4 +1,5 @@
-// Activations and weights to microscaled 4-bit codes, and back.  Both are one pass over memory.
+// Activations and weights to microscaled 4-bit codes, and back.  Both are one pass over memory: 8192 x 4608 with a mask there and back
+// 38.6 us, 3.9 TB/s of the 151 MB outside and 4.9 with the codes between (a copy moves 5.2).
 #include "vq_internal.h"
 #include "vq_mx4.h"
 

@@ -21,7 +21,7 @@ __device__ __forceinline__ void rotation(int position, float freq, float amplitu
 // A thread takes PAIRS neighbouring pairs of a token, computes their angles once and turns them in every `lanes_h`-th head, q's and
 // k's one after the other (threads behind the pairs copy as many channels that are not turned).  Neighbouring threads take
 // neighbouring pairs, then heads: a wavefront's accesses cover whole rows of a token.  Four pairs where the heads' turned part
-// divides by them, else two, else one: the second halves start at rot_dim / 2, and with them the accesses' alignment.
+// divides by them, else two, else one: the second halves start at rot_dim / 2, and with them the accesses' alignment.  (36 of 72 channels, out of place, 117 us, 18 159.)
 template <class TYPE, bool INTERLEAVED, int PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a) {
     const int pieces = a.copied_from + a.copied;       // per head: four pairs, or eight channels to copy
@@ -66,8 +66,8 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a) {
 #pragma unroll
         for (int e = 0; e < PAIRS; ++e) rotation(position, freq[e], a.amplitude, c[e], s[e]);
         const int half = a.rot_dim / 2;
-        // (kAtOnce heads' loads are on their way together: 32768 tokens, 16 + 16 heads of 72, halves 70 us with one, 65 so,
-        // 4.3 and 4.7 TB/s; neighbouring pairs 51.6 and 49.3)
+        // (kAtOnce heads' loads are on their way together: 32768 tokens, 16 + 16 heads of 72, halves 73.3 us with one, 70.0 so, 4.3 TB/s;
+        // neighbouring pairs 64.7 and 60.8, 5.0 TB/s; captured, inputs that are not in the caches)
         for (; h < heads; h += kAtOnce * a.lanes_h) {
             Piece in[kAtOnce];
 #pragma unroll
