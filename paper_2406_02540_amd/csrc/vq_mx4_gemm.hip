@@ -49,7 +49,9 @@ struct TileArgsMx {
     bool whole_lines;        // rows of Y start on memory lines
 };
 
-// ROWS16: rows of Y are whole 16-byte pieces (N % 8 == 0, Y on 16 bytes): range-checked stores.  Otherwise 64-bit addresses.
+// ROWS16: rows of Y are whole 16-byte pieces (N % 8 == 0, Y on 16 bytes): range-checked stores.  Otherwise 64-bit addresses, the same pieces
+// unaligned, and a row's last channels one by one: 1001 x 1184 -> 2821 12.9 us, 14.6 with the bias straight from memory and 64 bytes of a row
+// a store; 8192 x 1152 -> 4607 73 and 82 (4608 44, in tiles that this form has no registers for).
 template <class TYPE, class S, bool ROWS16>
 __global__ __launch_bounds__(64 * S::kWaves, 2) void mx4_gemm(TileArgsMx a) {
     __shared__ __align__(128) char lds[S::kLds];
@@ -92,7 +94,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void mx4_gemm(TileArgsMx a) {
         const int rows = min(M - row0, S::kTok), cols = min(N - col0, S::kCh);
         rx = make_rsrc(a.g.xq + (size_t)row0 * row_bytes, (unsigned)(rows * row_bytes));
         rw = make_rsrc(a.g.wq + (size_t)col0 * row_bytes, (unsigned)(cols * row_bytes));
-        rb = make_rsrc((const char*)a.g.bias + 2 * (size_t)col0, ROWS16 && a.g.bias ? 2u * cols : 0u);
+        rb = make_rsrc((const char*)a.g.bias + 2 * (size_t)col0, a.g.bias ? 2u * (cols & ~1) : 0u);       // (whole dwords)
         return true;
     };
     // Scales go through registers, sixteen of a row at a time for two stages: a touch of their line costs the caches as much as 128
@@ -155,9 +157,22 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void mx4_gemm(TileArgsMx a) {
         }
     };
     auto ask_bias = [&] {         // (every wavefront a turn: those beyond the bias write the same once more)
-        if (!ROWS16) return;
         const int turn = wave % (S::kBiasBytes / 256);
         load_to_lds_4(rb, base + S::kBias + bias_to * S::kBiasBytes + 256 * turn, 256 * turn + 4 * lane);
+    };
+
+    // Eight channels of a row that starts anywhere.
+    auto put = [&](T* y, int m, int n, int rows, int cols, v4u v) {
+        if (m >= rows) return;
+        T* const to = y + (size_t)m * N + n;
+        if (n + 8 <= cols) {
+            typedef v4u v4u_any __attribute__((aligned(2)));
+            *(v4u_any*)to = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (n + e < cols) ((unsigned short*)to)[e] = (unsigned short)(v[e >> 1] >> 16 * (e & 1));
+        }
     };
 
     v4f acc[S::TT][S::CC];
@@ -165,43 +180,52 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void mx4_gemm(TileArgsMx a) {
     auto finish = [&](int row, int col, int bias_from) {
         const int rows = min(M - row, S::kTok), cols = min(N - col, S::kCh);
         T* const y = (T*)a.g.y + (size_t)row * N + col;
-        if (ROWS16) {
-            const auto ry = __builtin_amdgcn_make_buffer_rsrc(y, 0, (int)(2 * ((unsigned)(rows - 1) * (unsigned)N + (unsigned)cols)), (int)kRsrcFlags);
-            const lds_bytes bias = (lds_bytes)lds + S::kBias + bias_from * S::kBiasBytes;
-            // A lane has eight channels of its token in each of two neighbouring pairs of blocks, 64 bytes of a token's row a store.  Lanes
-            // eight tokens apart exchange one of the two, and a store is 128 bytes of eight tokens: past the caches where these are whole
-            // lines (32768 x 1152 -> 4608 131 us, 147 through them, 8192 x 1152 -> 1152 16.6 and 20.3; halves of lines past the caches are slower than either),
-            // through them where rows start elsewhere and neighbouring stores share lines.
-            const bool low = r16 < 8;
+        const unsigned bytes = 2 * ((unsigned)(rows - 1) * (unsigned)N + (unsigned)cols);      // (meant for ROWS16 alone)
+        const auto ry = __builtin_amdgcn_make_buffer_rsrc(y, 0, (int)bytes, (int)kRsrcFlags);
+        const lds_bytes bias = (lds_bytes)lds + S::kBias + bias_from * S::kBiasBytes;
+        // A lane has eight channels of its token in each of two neighbouring pairs of blocks, 64 bytes of a token's row a store.  Lanes
+        // eight tokens apart exchange one of the two, and a store is 128 bytes of eight tokens: past the caches where these are whole
+        // lines (32768 x 1152 -> 4608 131 us, 147 through them, 8192 x 1152 -> 1152 16.6 and 20.3; halves of lines past the caches are slower than either),
+        // through them where rows start elsewhere and neighbouring stores share lines.
+        const bool low = r16 < 8;
 #pragma unroll
-            for (int c = 0; c < S::CC; c += 4) {
-                const int n = 16 * (S::CC * wc + c) + 8 * g;
-                float b[2][8];
+        for (int c = 0; c < S::CC; c += 4) {
+            const int n = 16 * (S::CC * wc + c) + 8 * g;
+            float b[2][8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const v4i b8 = *(__attribute__((address_space(3))) v4i*)(bias + 2 * (n + 32 * h));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) TYPE::unpack((unsigned)b8[e], b[h][2 * e], b[h][2 * e + 1]);
+                if (!ROWS16 && (cols & 1) && a.g.bias) {       // the last of an odd number is in no whole dword
+                    const int last = cols - 1 - (n + 32 * h);
+                    if (last >= 0 && last < 8) {
+                        const float its = (float)((const T*)a.g.bias)[col + cols - 1];
+#pragma unroll
+                        for (int e = 0; e < 8; e += 2) b[h][e] = e == last ? its : b[h][e];
+                    }
+                }
+            }
+            const int to = n + (low ? 0 : 32), m = 16 * S::TT * wt + (r16 & 7);
+            const int at = to < cols ? 2 * (m * N + to) : kNowhere;
+#pragma unroll
+            for (int t = 0; t < S::TT; ++t) {
+                v4u piece[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const v4i b8 = *(__attribute__((address_space(3))) v4i*)(bias + 2 * (n + 32 * h));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) TYPE::unpack((unsigned)b8[e], b[h][2 * e], b[h][2 * e + 1]);
+                    const v4f lo = acc[t][c + 2 * h], hi = acc[t][c + 2 * h + 1];
+                    piece[h] = v4u{TYPE::pack(lo[0] + b[h][0], lo[1] + b[h][1]), TYPE::pack(lo[2] + b[h][2], lo[3] + b[h][3]),
+                                   TYPE::pack(hi[0] + b[h][4], hi[1] + b[h][5]), TYPE::pack(hi[2] + b[h][6], hi[3] + b[h][7])};
                 }
-                const int to = n + (low ? 0 : 32);
-                const int at = to < cols ? 2 * ((16 * S::TT * wt + (r16 & 7)) * N + to) : kNowhere;
+                v4u first, second;
 #pragma unroll
-                for (int t = 0; t < S::TT; ++t) {
-                    v4u piece[2];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const v4f lo = acc[t][c + 2 * h], hi = acc[t][c + 2 * h + 1];
-                        piece[h] = v4u{TYPE::pack(lo[0] + b[h][0], lo[1] + b[h][1]), TYPE::pack(lo[2] + b[h][2], lo[3] + b[h][3]),
-                                       TYPE::pack(hi[0] + b[h][4], hi[1] + b[h][5]), TYPE::pack(hi[2] + b[h][6], hi[3] + b[h][7])};
-                    }
-                    v4u first, second;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const unsigned given = low ? piece[1][e] : piece[0][e];
-                        const unsigned taken = (unsigned)__builtin_amdgcn_mov_dpp((int)given, 0x128, 0xF, 0xF, true);    // row_ror:8
-                        first[e] = low ? piece[0][e] : taken;
-                        second[e] = low ? taken : piece[1][e];
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned given = low ? piece[1][e] : piece[0][e];
+                    const unsigned taken = (unsigned)__builtin_amdgcn_mov_dpp((int)given, 0x128, 0xF, 0xF, true);    // row_ror:8
+                    first[e] = low ? piece[0][e] : taken;
+                    second[e] = low ? taken : piece[1][e];
+                }
+                if (ROWS16) {
                     const int at_first = to < cols ? at + 32 * t * N : kNowhere, at_second = to < cols ? at + 32 * t * N + 16 * N : kNowhere;
                     if (a.whole_lines) {
                         __builtin_amdgcn_raw_buffer_store_b128(first, ry, at_first, 0, 2 /* nontemporal */);
@@ -210,31 +234,9 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void mx4_gemm(TileArgsMx a) {
                         __builtin_amdgcn_raw_buffer_store_b128(first, ry, at_first, 0, 0);
                         __builtin_amdgcn_raw_buffer_store_b128(second, ry, at_second, 0, 0);
                     }
-                }
-            }
-        } else {
-            const T* const bias = (const T*)a.g.bias + col;
-#pragma unroll
-            for (int c = 0; c < S::CC; c += 2) {
-                const int n = 16 * (S::CC * wc + c) + 8 * g;
-                float b[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) b[e] = a.g.bias && n + e < cols ? (float)bias[n + e] : 0.0f;
-#pragma unroll
-                for (int t = 0; t < S::TT; ++t) {
-                    const int m = 16 * (S::TT * wt + t) + r16;
-                    if (m >= rows) continue;
-                    const v4f lo = acc[t][c], hi = acc[t][c + 1];
-                    T* const to = y + (size_t)m * N + n;
-                    if (n + 8 <= cols) {
-                        typedef v4i v4i_any __attribute__((aligned(2)));
-                        *(v4i_any*)to = v4i{(int)TYPE::pack(lo[0] + b[0], lo[1] + b[1]), (int)TYPE::pack(lo[2] + b[2], lo[3] + b[3]),
-                                            (int)TYPE::pack(hi[0] + b[4], hi[1] + b[5]), (int)TYPE::pack(hi[2] + b[6], hi[3] + b[7])};
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (n + e < cols) to[e] = (T)((e < 4 ? lo[e & 3] : hi[e & 3]) + b[e]);
-                    }
+                } else {
+                    put(y, m + 16 * t, to, rows, cols, first);
+                    put(y, m + 16 * t + 8, to, rows, cols, second);
                 }
             }
         }
