@@ -12,7 +12,7 @@
 //
 // Measured (captured, several hundred MB of inputs and outputs in turn, so that none is in the caches): 32768 x 1152 -> 4608 131 us (2.7
 // PFLOP/s; its 324 MB alone are 63 us at the 5.2 TB/s of a copy), 32768 x 4608 -> 1152 133, 8192 x 1152 -> 1152 16.6, 8192 x 8192 -> 8192
-// 277 (4.0 PFLOP/s).  Where K is long the matrix units are busy 42 % of the time at 2.07 GHz; where it is short a tile's outputs cost
+// 277 (4.0 PFLOP/s).  At the last the matrix units were busy 42 % of the time at 2.07 GHz (counted before the stores' last form); where K is short a tile's outputs cost
 // as much as its products.
 #include "vq_internal.h"
 #include "vq_mx4_product.h"
