@@ -343,7 +343,8 @@ size_t vq_linear_mx4_workspace_bytes(int M, int N, int K);
  * heads are any number of elements apart (the channels of a head are contiguous), so that
  * slices of the QKV layer's output go in as they are.  Strides are in elements and multiples
  * of 8 (inputs: 0 too, for a row that all tokens or heads share; tokens of k and v at most 2^23
- * apart), pointers on 16 bytes (positions, cu_q, cu_k on 4), dtype VQ_F16 or VQ_BF16.
+ * apart), pointers on 16 bytes (positions, cu_q, cu_k on 4), dtype VQ_F16 or VQ_BF16.  An output
+ * two of whose rows (token, head) share memory is VQ_ERR_SHAPE.
  *
  * vq_rotary: rotary positions.  For pair i of a head's first rot_dim channels and the token's
  *   position p:  angle = p * inv_freq[i],  c = amplitude * cos(angle),  s = amplitude * sin(angle),

@@ -231,13 +231,27 @@ int validate_mx4_gemm(const void* xq, const void* x_scale, const void* wq, const
     return VQ_OK;
 }
 
-// A view's two strides in elements: heads and rows start on 16 bytes, what is written lies apart.
-bool strides_ok(const int64_t* s, int tokens, int heads, int head_dim, bool written) {
-    for (int i = 0; i < 2; ++i) {
-        if (s[i] < 0 || s[i] % 8 != 0 || s[i] > (int64_t)1 << 40) return false;
-        if (written && s[i] < head_dim && (i == 0 ? tokens : heads) > 1) return false;
+// Whether no two of the rows (token, head) of a view share memory; its strides are not negative.
+bool rows_apart(const int64_t* s, int tokens, int heads, int head_dim) {
+    if ((tokens > 1 && s[0] < head_dim) || (heads > 1 && s[1] < head_dim)) return false;
+    if (tokens <= 1 || heads <= 1) return true;
+    // the few along one axis, the many along the other: a row of one either spans the other's rows, or lies between them
+    const bool few_heads = heads <= tokens;
+    const int64_t few = few_heads ? heads : tokens, many = few_heads ? tokens : heads;
+    const int64_t a = s[few_heads], b = s[!few_heads];
+    if (b >= (few - 1) * a + head_dim || (a - head_dim) / b >= many - 1) return true;
+    for (int64_t i = 1; i < few; ++i) {      // (at most 2^16 of them, in layouts that are neither)
+        const int64_t below = i * a / b, gap = i * a - below * b;
+        if ((below < many && gap < head_dim) || (below + 1 < many && b - gap < head_dim)) return false;
     }
     return true;
+}
+
+// A view's two strides in elements: heads and rows start on 16 bytes, what is written lies apart.
+bool strides_ok(const int64_t* s, int tokens, int heads, int head_dim, bool written) {
+    for (int i = 0; i < 2; ++i)
+        if (s[i] < 0 || s[i] % 8 != 0 || s[i] > (int64_t)1 << 40) return false;
+    return !written || rows_apart(s, tokens, heads, head_dim);
 }
 constexpr int64_t kMaxKeyStride = 1 << 23;   // a tile's offsets are 32-bit
 constexpr int kMaxRows = 0x7FFFFF00;         // rows and keys of a last tile fit an int

@@ -248,3 +248,28 @@ def test_the_definition_of_attention():
     s = torch.einsum("hd,khd->hk", q[3].double(), k[1:6].double().repeat_interleave(2, 1)) * 0.3
     want = torch.einsum("hk,khd->hd", s.softmax(1), v[1:6].double().repeat_interleave(2, 1))
     assert torch.allclose(out[3], want) and (off >= 0).all()
+
+
+def test_written_rows_that_share_memory_are_refused(lib):
+    def rotary(T, H, D, token, head, k_out=False):
+        own, dense = (H * D, D), (token, head)
+        s = own + own + own + dense if k_out else own + dense + own + own
+        return lib.vq_rotary(P(A), P(1 << 40), P(A), P(1 << 50), 0, P(A), P(A), F(1.0), 0, T, H, H, D, D, _strides(*s), None)
+
+    def attention(T, H, D, token, head):
+        s = (H * D, D) * 3 + (token, head)
+        return lib.vq_attention(P(A), P(A), P(A), P(1 << 40), 0, P(A), P(A), 1, T, 1, H, H, D, _strides(*s), F(0.1), 0, None, 0, None)
+
+    def both(*sizes):
+        got = {attention(*sizes), rotary(*sizes), rotary(*sizes, k_out=True)}
+        assert len(got) == 1
+        return got.pop()
+
+    # token t + 1, head h is token t, head h + 1; rows of neighbours overlap in part; far ones meet
+    shared = [(4, 8, 128, 128, 128), (600, 8, 64, 128, 64), (600, 8, 64, 64, 128), (3, 2, 64, 64, 96), (3, 4, 8, 24, 16), (4, 3, 8, 16, 24),
+              (1 << 20, 2, 8, 8, 8 * ((1 << 20) - 1)), (65536, 16, 8, 16, 8), (4, 65, 8, 512, 8), (1002, 1002, 8, 8008, 8000)]
+    assert [both(*s) for s in shared] == [SHAPE] * len(shared)
+    # token-major, head-major, with gaps, one token, one head, and rows that lie between each other's
+    apart = [(600, 8, 64, 512, 64), (600, 8, 64, 64, 600 * 64), (600, 8, 64, 1024, 72), (1, 8, 64, 8, 64), (600, 1, 64, 64, 0), (3, 3, 8, 24, 16),
+             (1 << 20, 2, 8, 8, 8 << 20), (65536, 2, 8, 16, 8), (4, 64, 8, 512, 8), (1000, 1000, 8, 8008, 8000), (1000, 1000, 8, 8008, 8), (2, 1000, 8, 8, 16), (2, 2, 8, 1 << 40, 1 << 39)]
+    assert [both(*s) for s in apart] == [ARCH] * len(apart)
