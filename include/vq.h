@@ -310,7 +310,8 @@ int vq_quantize_weight(const float* w_f32, const float* chan_s, int w_bits, void
  *           bit 3 of a code is its sign, bits 0..2 number the magnitudes above
  *   scales  uint8 [M,S], S = VQ_MX4_SCALE_STRIDE(K): byte b of a row is E + 127 of block b, the
  *           bytes behind the last block are written as 0 and not looked at by the readers
- * K % 32 == 0, K <= VQ_MAX_K and pointers on 16 bytes, for every entry point here.
+ * K % 32 == 0, K <= VQ_MAX_K and pointers on 16 bytes, for every entry point here; for the product and the
+ * layer M and N at most 2^31 - 256, and y at most 2^31 - 4096 tiles of 64 x 128.
  *
  * vq_mx4_quantize:   x [M,K] of type dtype (VQ_F16, VQ_BF16; VQ_F32 for weights), chan_mul fp32
  *                    [K] or NULL: Eq. 3's 1/s for activations, s for weights.
@@ -334,7 +335,7 @@ int vq_gemm_mx4(const uint8_t* xq, const uint8_t* x_scale, const uint8_t* wq, co
                 const void* bias, void* y, int dtype, int M, int N, int K, void* hip_stream);
 int vq_linear_mx4(const void* x, const float* chan_mul, const uint8_t* wq, const uint8_t* w_scale, const void* bias,
                   void* y, int dtype, void* workspace, size_t workspace_bytes, int M, int N, int K, void* hip_stream);
-/* Bytes of workspace vq_linear_mx4 needs (0 if a size is invalid).  Host-only, no HIP call. */
+/* Bytes of workspace vq_linear_mx4 needs (0 if a size is negative or K none of those above).  Host-only, no HIP call. */
 size_t vq_linear_mx4_workspace_bytes(int M, int N, int K);
 
 /*

@@ -96,6 +96,7 @@ struct Mx4GemmArgs {
 // dividing K (vq_mx4_gemm_split.hip: 32 x 32, 48 x 48, 32 x 64).
 struct Mx4Choice { int tile_t, tile_c; bool divide_k; };
 Mx4Choice choose_mx4_gemm(int M, int N, int K, int num_cus);
+bool mx4_gemm_takes(int M, int N);      // whether launch_mx4_gemm has a kernel for these sizes
 hipError_t launch_mx4_gemm(const Mx4GemmArgs& a, int dtype, int num_cus, hipStream_t stream);
 hipError_t launch_mx4_gemm_lines(int tile_t, int tile_c, const Mx4GemmArgs& a, int dtype, hipStream_t stream);
 // A layer of few tokens in one launch, from x instead of xq; small_mx4_layer: whether it is the faster way.

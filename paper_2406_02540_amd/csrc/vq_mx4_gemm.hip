@@ -339,12 +339,10 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void mx4_gemm(TileArgsMx a) {
 template <class S>
 hipError_t launch(const Mx4GemmArgs& g, int dtype, int num_cus, hipStream_t stream) {
     TileArgsMx a{g, 0, 0, 0, 0, 0, g.N % 64 == 0 && (uintptr_t)g.y % 128 == 0};
-    if (g.M > 0x7FFFFF00 || g.N > 0x7FFFFF00) return hipErrorInvalidValue;     // (rows and channels of a last tile fit an int)
+    if (!mx4_gemm_takes(g.M, g.N)) return hipErrorInvalidValue;
     a.tiles_t = (g.M + S::kTok - 1) / S::kTok;
     a.tiles_c = (g.N + S::kCh - 1) / S::kCh;
-    const long tiles = (long)a.tiles_t * a.tiles_c;
-    if (tiles > 0x7FFFFF0l || (long)kBand * a.tiles_c > 0x7FFFFFFFl) return hipErrorInvalidValue;
-    a.tiles = (int)tiles;
+    a.tiles = (int)((long)a.tiles_t * a.tiles_c);
     a.tiles_per_xcd = (a.tiles + kXcds - 1) / kXcds;
     const int resident = (int)(163840 / S::kLds) * (num_cus >= kXcds ? num_cus / kXcds : 1);
     a.slots = a.tiles_per_xcd < resident ? a.tiles_per_xcd : resident;
@@ -357,6 +355,12 @@ hipError_t launch(const Mx4GemmArgs& g, int dtype, int num_cus, hipStream_t stre
 }
 
 }  // namespace
+
+// Rows and channels of a last tile fit an int, and so do the numbers of the smallest tiles, 64 x 128, and those that a workgroup asks for behind its last.
+bool mx4_gemm_takes(int M, int N) {
+    static_assert((0x7FFFFF00l + 127) / 128 * kBand <= 0x7FFFFFFFl, "tiles of a band");
+    return M <= 0x7FFFFF00 && N <= 0x7FFFFF00 && (((long)M + 63) / 64) * (((long)N + 127) / 128) <= 0x7FFFF000l;
+}
 
 // The kernel for a product's sizes, by what each would take: rounds of its workgroups on the chip times a workgroup's time, fitted to
 // measurements over M 1 .. 32768, N 1152 .. 8192, K 1152 .. 8192 (us; off by 10 to 15 %).  Where the wavefronts divide K, a

@@ -156,7 +156,7 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_gemm_lines(Mx4GemmArgs a) {
 template <class TYPE, int TT, int CC, int WAVES, XFrom X_FROM>
 hipError_t launch_lines(const Mx4GemmArgs& a, hipStream_t stream) {
     const long tiles = (((long)a.M - 1) / (16 * TT) + 1) * (((long)a.N - 1) / (16 * CC) + 1);
-    if (a.M > 0x7FFFFF00 || a.N > 0x7FFFFF00 || tiles * 64 * WAVES >= 1l << 32) return hipErrorInvalidValue;
+    if (!mx4_gemm_takes(a.M, a.N) || tiles * 64 * WAVES >= 1l << 32) return hipErrorInvalidValue;
     return enqueue(mx4_gemm_lines<TYPE, TT, CC, WAVES, X_FROM>, dim3((unsigned)tiles), dim3(64 * WAVES), stream, a);
 }
 

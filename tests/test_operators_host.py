@@ -273,3 +273,18 @@ def test_written_rows_that_share_memory_are_refused(lib):
     apart = [(600, 8, 64, 512, 64), (600, 8, 64, 64, 600 * 64), (600, 8, 64, 1024, 72), (1, 8, 64, 8, 64), (600, 1, 64, 64, 0), (3, 3, 8, 24, 16),
              (1 << 20, 2, 8, 8, 8 << 20), (65536, 2, 8, 16, 8), (4, 64, 8, 512, 8), (1000, 1000, 8, 8008, 8000), (1000, 1000, 8, 8008, 8), (2, 1000, 8, 8, 16), (2, 2, 8, 1 << 40, 1 << 39)]
     assert [both(*s) for s in apart] == [ARCH] * len(apart)
+
+
+def test_microscaled_products_that_no_launch_takes_are_refused_up_front(lib):
+    # (on an error nothing was enqueued: the layer may not find out behind its quantizer)
+    def g(M, N, K=32):
+        return lib.vq_gemm_mx4(P(A), P(A), P(A), P(A), None, P(A), 0, M, N, K, None)
+
+    def l(M, N, K=32):
+        return lib.vq_linear_mx4(P(A), None, P(A), P(A), None, P(A), 0, P(A), 1 << 62, M, N, K, None)
+
+    most = 2**31 - 256
+    for f in (g, l):
+        assert [f(most + 1, 8), f(2**31 - 1, 1), f(8, most + 1), f(1, 2**31 - 1), f(most, most), f(1 << 25, 1 << 20)] == [SHAPE] * 6
+        # (134 million tiles and more)
+        assert [f(most, 8), f(8, most), f(1 << 20, 1 << 21), f(1 << 24, 1 << 19)] == [ARCH] * 4
