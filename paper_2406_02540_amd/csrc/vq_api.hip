@@ -223,8 +223,9 @@ int validate_mx4(int M, int K) { return M < 0 || K <= 0 || K > VQ_MAX_K || K % V
 int validate_mx4_gemm(const void* xq, const void* x_scale, const void* wq, const void* w_scale, const void* bias, const void* y,
                       int dtype, int M, int N, int K) {
     if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
-    if (N < 0 || validate_mx4(M, K) != VQ_OK || !vq::mx4_gemm_takes(M, N)) return VQ_ERR_SHAPE;
+    if (N < 0 || validate_mx4(M, K) != VQ_OK) return VQ_ERR_SHAPE;
     if (M == 0 || N == 0) return VQ_OK;
+    if (!vq::mx4_gemm_takes(M, N)) return VQ_ERR_SHAPE;
     if (!xq || !x_scale || !wq || !w_scale || !y) return VQ_ERR_NULL;
     if (misaligned(xq) || misaligned(x_scale) || misaligned(wq) || misaligned(w_scale) || misaligned(y) || (bias && misaligned(bias)))
         return VQ_ERR_ALIGN;
@@ -529,8 +530,9 @@ size_t vq_linear_mx4_workspace_bytes(int M, int N, int K) {
 int vq_linear_mx4(const void* x, const float* chan_mul, const uint8_t* wq, const uint8_t* w_scale, const void* bias, void* y,
                   int dtype, void* workspace, size_t workspace_bytes, int M, int N, int K, void* hip_stream) {
     if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
-    if (N < 0 || validate_mx4(M, K) != VQ_OK || !vq::mx4_gemm_takes(M, N)) return VQ_ERR_SHAPE;
+    if (N < 0 || validate_mx4(M, K) != VQ_OK) return VQ_ERR_SHAPE;
     if (M == 0 || N == 0) return VQ_OK;
+    if (!vq::mx4_gemm_takes(M, N)) return VQ_ERR_SHAPE;
     if (!workspace || !x) return VQ_ERR_NULL;
     if (misaligned(workspace) || misaligned(x) || (chan_mul && misaligned(chan_mul))) return VQ_ERR_ALIGN;
     if (workspace_bytes < vq_linear_mx4_workspace_bytes(M, N, K)) return VQ_ERR_WORKSPACE;

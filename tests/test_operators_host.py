@@ -286,5 +286,6 @@ def test_microscaled_products_that_no_launch_takes_are_refused_up_front(lib):
     most = 2**31 - 256
     for f in (g, l):
         assert [f(most + 1, 8), f(2**31 - 1, 1), f(8, most + 1), f(1, 2**31 - 1), f(most, most), f(1 << 25, 1 << 20)] == [SHAPE] * 6
+        assert [f(0, 2**31 - 1), f(2**31 - 1, 0)] == [OK] * 2
         # (134 million tiles and more)
         assert [f(most, 8), f(8, most), f(1 << 20, 1 << 21), f(1 << 24, 1 << 19)] == [ARCH] * 4
