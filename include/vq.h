@@ -369,7 +369,9 @@ size_t vq_linear_mx4_workspace_bytes(int M, int N, int K);
  *
  * vq_attention: out = softmax(softmax_scale * q k^T) v over packed sequences.
  *     q, out     [Tq, heads, head_dim]; k, v [Tk, kv_heads, head_dim]; heads % kv_heads == 0, head h
- *                reads head h / (heads / kv_heads) of k and v; Tq * heads and Tk at most 2^31 - 256
+ *                reads head h / (heads / kv_heads) of k and v; Tq * heads and Tk at most 2^31 - 256, heads at most 2^16,
+ *                and Tq * heads / 128 + (sequences + 8) * kv_heads below 2^24 (beyond it VQ_ERR_SHAPE where a
+ *                launch does not hold the workgroups)
  *     cu_q, cu_k int32 [sequences + 1], ascending: sequence b has the query rows cu_q[b] ..
  *                cu_q[b+1] - 1 and the key rows cu_k[b] .. cu_k[b+1] - 1; the numbers may differ
  *                (cross attention, new tokens behind earlier ones) and may be 0

@@ -613,8 +613,9 @@ size_t vq_attention_workspace_bytes(int sequences, int Tq, int Tk, int heads, in
         head_dim % 8 != 0 || head_dim > VQ_MAX_HEAD_DIM)
         return 0;
     if ((int64_t)Tq * heads > kMaxRows || Tk > kMaxRows) return 0;
-    const size_t parts = (size_t)1 << vq::attention_split_shift(sequences, Tq, Tk, heads, kv_heads);
-    return parts == 1 ? 0 : parts * (size_t)Tq * (size_t)heads * (size_t)(head_dim + 2) * sizeof(float);
+    const vq::AttentionChoice choice = vq::choose_attention(sequences, Tq, Tk, heads, kv_heads);
+    const size_t parts = (size_t)1 << choice.split_shift;
+    return parts == 1 || !choice.fits ? 0 : parts * (size_t)Tq * (size_t)heads * (size_t)(head_dim + 2) * sizeof(float);
 }
 
 int vq_attention(const void* q, const void* k, const void* v, void* out, int dtype, const int32_t* cu_q, const int32_t* cu_k,
@@ -626,6 +627,8 @@ int vq_attention(const void* q, const void* k, const void* v, void* out, int dty
         !(softmax_scale >= 1e-30f && softmax_scale <= 1e30f))
         return VQ_ERR_SHAPE;
     if (sequences == 0 || Tq == 0) return VQ_OK;
+    const vq::AttentionChoice choice = vq::choose_attention(sequences, Tq, Tk, heads, kv_heads);
+    if (!choice.fits) return VQ_ERR_SHAPE;
     if (!q || !out || !cu_q || !cu_k || !strides || (Tk > 0 && (!k || !v))) return VQ_ERR_NULL;
     for (int i = 0; i < 4; ++i) {
         const bool keys = i == 1 || i == 2;
@@ -650,10 +653,10 @@ int vq_attention(const void* q, const void* k, const void* v, void* out, int dty
     a.v_token = strides[4], a.v_head = strides[5], a.o_token = strides[6], a.o_head = strides[7];
     a.scale_log2 = (float)((double)softmax_scale * 1.44269504088896340736);
     a.group_shift = (a.group & (a.group - 1)) == 0 ? __builtin_ctz(a.group) : -1;
-    a.split_shift = vq::attention_split_shift(sequences, Tq, Tk, heads, kv_heads);
+    a.split_shift = choice.split_shift;
     a.part_o = (float*)workspace;
     a.part_ml = a.part_o ? a.part_o + ((size_t)Tq << a.split_shift) * heads * head_dim : nullptr;
-    return launch_status(vq::launch_attention(a, dtype, (hipStream_t)hip_stream));
+    return launch_status(vq::launch_attention(a, choice.kernel, dtype, (hipStream_t)hip_stream));
 }
 
 const char* vq_status_string(int status) {

@@ -69,14 +69,13 @@ __device__ __forceinline__ bool place_of(const AttentionArgs& a, int& kv, int& i
     }
     return item < a.items;
 }
-// The workgroups that place_of() has in mind, or 0: more than a launch takes.
-inline unsigned attention_grid(AttentionArgs& a, long tiles, int threads) {
-    const long items = tiles << a.split_shift, blocks = (items + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds * a.kv_heads;
-    if (items > 0x7FFFFF00 || blocks * threads >= 1l << 32) return 0;
+// The workgroups that place_of() has in mind (choose_attention() has seen that a launch takes them).
+inline unsigned attention_grid(AttentionArgs& a, long tiles) {
     a.tiles = (int)tiles;
-    a.items = (int)items;
+    a.items = (int)(tiles << a.split_shift);
     a.heads_together = a.Tk / a.sequences <= 512 && a.head_dim % 64 != 0;
-    return (unsigned)(a.heads_together ? blocks : items * a.kv_heads);
+    const long items = a.heads_together ? ((long)a.items + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds : a.items;
+    return (unsigned)(items * a.kv_heads);
 }
 
 // ---- tiles of K and V in LDS ---------------------------------------------------------------------------------

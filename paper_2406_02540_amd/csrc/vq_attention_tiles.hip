@@ -224,8 +224,7 @@ __global__ __launch_bounds__(64 * kWaves, CHUNKS == 16 ? 2 : 3) void attention_t
 
 template <class TYPE>
 hipError_t launch(AttentionArgs a, hipStream_t stream) {
-    const unsigned blocks = attention_grid(a, attention_items(a.sequences, a.Tq, a.group), 64 * kWaves);
-    if (!blocks) return hipErrorInvalidValue;
+    const unsigned blocks = attention_grid(a, attention_items(a.sequences, a.Tq, a.group));
     void (*kernel)(AttentionArgs) = a.head_dim <= 64   ? attention_tiles<TYPE, 8, 4>
                                     : a.head_dim <= 80 ? attention_tiles<TYPE, 12, 5>
                                     : a.head_dim <= 96 ? attention_tiles<TYPE, 12, 6>

@@ -136,16 +136,18 @@ struct AttentionArgs {
     int items;                // these for every part of their keys,
     int heads_together;       // and whether an item's heads of K and V go to one XCD, or a head's items
 };
-// The logarithm of the workgroups that divide the keys of a tile, from the sizes alone.  Tq * heads < 2^31.
-int attention_split_shift(int sequences, int Tq, int Tk, int heads, int kv_heads);
-hipError_t launch_attention(const AttentionArgs& a, int dtype, hipStream_t stream);
-// Its two kernels: few query rows a sequence (vq_attention.hip), or tiles of kTileRows (vq_attention_tiles.hip), at most
-// attention_items() of them for a head of K and V.
+// Its kernels: tiles of kTileRows query rows (vq_attention_tiles.hip), at most attention_items() of them for a head of K and V, or few rows a
+// sequence (vq_attention.hip), by four wavefronts or by one; and how often the keys of a tile are divided among workgroups, from the
+// sizes alone.  Tq * heads < 2^31.
+enum AttentionKernel { kAttentionTiles = 0, kAttentionRows = 1, kAttentionRowsAlone = 2 };
+struct AttentionChoice {
+    AttentionKernel kernel;
+    int split_shift;          // the logarithm of the workgroups that divide the keys
+    bool fits;                // in one launch
+};
+AttentionChoice choose_attention(int sequences, int Tq, int Tk, int heads, int kv_heads);
+hipError_t launch_attention(const AttentionArgs& a, AttentionKernel kernel, int dtype, hipStream_t stream);
 constexpr int kTileRows = 128;
-// Rows of the average sequence: up to 32, one MFMA block of them.  With all in tiles 16 single tokens over long keys take 230 us instead
-// of 170 and 2048 sequences of 16 239 instead of 84 (64 equal ones over 4096 keys 191 and 215); with up to 64 by rows 16 sequences of 64 rows over
-// 4096 keys 151 instead of 71 and 512 sequences of 64 91 instead of 75.
-inline bool attention_by_rows(int sequences, int Tq, int group) { return (long)Tq * group <= 32l * sequences; }
 inline long attention_items(int sequences, int Tq, int group) { return (long)Tq * group / kTileRows + sequences; }
 hipError_t launch_attention_tiles(const AttentionArgs& a, int dtype, hipStream_t stream);
 
@@ -155,4 +157,5 @@ hipError_t launch_attention_tiles(const AttentionArgs& a, int dtype, hipStream_t
 // writes its rows (Out, vq_gemm_common.h).  Not a part of vq.h.
 extern "C" void vq_internal_gemm_choice(int w_bits, int M, int N, int K, int num_cus, int choice[3]);
 extern "C" void vq_internal_mx4_choice(int M, int N, int K, int num_cus, int choice[3]);
+extern "C" void vq_internal_attention_choice(int sequences, int Tq, int Tk, int heads, int kv_heads, int choice[2]);
 extern "C" int vq_internal_gemm_out(int N, const void* y, const void* acc_out);

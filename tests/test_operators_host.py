@@ -289,3 +289,19 @@ def test_microscaled_products_that_no_launch_takes_are_refused_up_front(lib):
         assert [f(0, 2**31 - 1), f(2**31 - 1, 0)] == [OK] * 2
         # (134 million tiles and more)
         assert [f(most, 8), f(8, most), f(1 << 20, 1 << 21), f(1 << 24, 1 << 19)] == [ARCH] * 4
+
+
+def test_attention_that_no_launch_takes_is_refused_up_front(lib):
+    def a(B, Tq, Tk, H, G):
+        s = (8, 8) * 3 + (64 * H, 64)
+        need = lib.vq_attention_workspace_bytes(B, Tq, Tk, H, G, 64)
+        return lib.vq_attention(P(A), P(A), P(A), P(1 << 50), 0, P(A), P(A), B, Tq, Tk, H, G, 64, _strides(*s), F(0.1), 0, P(A), need, None)
+
+    most = 2**31 - 256
+    # workgroups of 2^32 threads and more: rows by the tile, rows by the sequence, by a wavefront a sequence
+    beyond = [(1, most // 64, 2000, 64, 64), (3000, most, most, 1, 1), (1 << 21, 1 << 21, most, 8, 8), (1 << 25, 1 << 25, 1 << 25, 2, 2)]
+    assert [a(*s) for s in beyond] == [SHAPE] * len(beyond)
+    assert [lib.vq_attention_workspace_bytes(*s, 64) for s in beyond] == [0] * len(beyond)
+    within = [(1, 1 << 24, 2000, 64, 64), (1, most - 4096, 2000, 1, 1), (1000, 1 << 30, most, 1, 1), ((1 << 21) - 8, 1 << 21, most, 8, 8),
+              ((1 << 25) - 8, 1 << 25, 1 << 25, 2, 2), (1, 1, most, 1 << 16, 1)]
+    assert [a(*s) for s in within] == [ARCH] * len(within)
