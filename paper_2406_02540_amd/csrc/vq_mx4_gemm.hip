@@ -43,6 +43,14 @@ struct Shape {
     static_assert(kBiasBytes / 4 % 64 == 0 && kBiasBytes / 256 <= kWaves && CC % 2 == 0, "whole loads of the bias");
 };
 
+// Where channel `to` of row m of a tile is, in bytes, where stores are range-checked (N below 2^21).  0 for rows that start anywhere:
+// those are addressed in 64 bits, and with their N the product may not fit (an overflow is undefined even where nothing uses it).
+template <bool ROWS16>
+__host__ __device__ constexpr int checked_at(int m, int N, int to) {
+    return ROWS16 ? 2 * (m * N + to) : 0;
+}
+static_assert(checked_at<true>(255, (1 << 21) - 1, 255) > 0 && checked_at<false>(255, 0x7FFFFFFF, 255) == 0, "nothing overflows");
+
 struct TileArgsMx {
     Mx4GemmArgs g;
     int tiles_t, tiles_c, tiles, tiles_per_xcd, slots;
@@ -207,7 +215,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void mx4_gemm(TileArgsMx a) {
                 }
             }
             const int to = n + (low ? 0 : 32), m = 16 * S::TT * wt + (r16 & 7);
-            const int at = to < cols ? 2 * (m * N + to) : kNowhere;
+            const int at = to < cols ? checked_at<ROWS16>(m, N, to) : kNowhere;
 #pragma unroll
             for (int t = 0; t < S::TT; ++t) {
                 v4u piece[2];

@@ -51,3 +51,10 @@ def test_kernels_do_not_spill(source):
     scratch = [int(b) for b in re.findall(r"ScratchSize \[bytes/lane\]: (\d+)", out.stderr)]
     assert len(names) == len(scratch) > 0
     assert {n: b for n, b in zip(names, scratch) if b} == {}
+
+
+def test_wide_rows_reach_the_stores_of_any_row():
+    pytest.importorskip("torch")
+    from test_gpu_mx4_wide import WIDE
+    assert all(N >= 1 << 21 and not choice(M, N, K)[2] for M, N, K in WIDE)
+    assert any(N % 8 == 0 for _, N, _ in WIDE) and any(2 * N * min(M, choice(M, N, K)[0]) >= 1 << 31 for M, N, K in WIDE)
