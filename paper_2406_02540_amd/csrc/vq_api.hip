@@ -597,7 +597,8 @@ int vq_rotary_frequencies(float* inv_freq, float* amplitude, int rot_dim, double
     if (scaling == VQ_ROPE_PARTS) {
         low = std::fmax(std::floor(pair_of(32.0)), 0.0);
         high = std::fmin(std::ceil(pair_of(1.0)), rot_dim - 1.0);
-        if (high <= low) high = low + 0.001;
+        if (high <= 0) low = -1.0, high = 0.0;          // (no pair turns more than once)
+        else if (high <= low) high = low + 0.001;       // (every pair turns more than 32 times)
     }
     for (int i = 0; i < rot_dim / 2; ++i) {
         const double f = std::pow(base, -2.0 * i / rot_dim);

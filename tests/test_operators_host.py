@@ -305,3 +305,19 @@ def test_attention_that_no_launch_takes_is_refused_up_front(lib):
     within = [(1, 1 << 24, 2000, 64, 64), (1, most - 4096, 2000, 1, 1), (1000, 1 << 30, most, 1, 1), ((1 << 21) - 8, 1 << 21, most, 8, 8),
               ((1 << 25) - 8, 1 << 25, 1 << 25, 2, 2), (1, 1, most, 1 << 16, 1)]
     assert [a(*s) for s in within] == [ARCH] * len(within)
+
+
+@pytest.mark.parametrize("R,base,factor", [(64, 10000.0, 8.0), (128, 5e5, 32.0), (2, 10000.0, 4.0), (72, 100.0, 1.5)])
+@pytest.mark.parametrize("length", [1, 4, 6, 7, 40, 201, 202, 4096, 1 << 30])
+def test_frequencies_by_parts_follow_the_turns(R, base, factor, length):
+    import paper_2406_02540_amd as vq
+    f, _ = vq.vq_rotary_frequencies(R, base, "parts", factor, length)
+    plain = [base ** (-2 * i / R) for i in range(R // 2)]
+    turns = [length * v / (2 * math.pi) for v in plain]
+    for i, (v, p, n) in enumerate(zip(f.tolist(), plain, turns)):
+        if n > 32:
+            assert v == pytest.approx(p, rel=1e-6), (i, n)
+        elif n < 1 and (i == 0 or turns[i - 1] < 1):       # (the blend ends at a whole pair)
+            assert v == pytest.approx(p / factor, rel=1e-6), (i, n)
+        else:
+            assert p / factor * 0.999999 <= v <= p * 1.000001, (i, n)
