@@ -34,10 +34,13 @@ def log(*a):
 
 
 def csrc_hash():
-    """Identifies the kernel sources a counter summary under profiles/ was taken with."""
+    """Identifies the kernel sources a counter summary under profiles/ was taken with: those of the int8 kernels that this
+    program times, whatever other operators the library has."""
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2406_02540_amd", "csrc")
-    for f in sorted(glob.glob(os.path.join(d, "*.hip")) + glob.glob(os.path.join(d, "*.h"))):
+    kernels = ("vq_quantize", "vq_fused", "vq_gemm", "vq_linear", "vq_lanes")
+    for f in sorted(f for f in glob.glob(os.path.join(d, "*.hip")) + glob.glob(os.path.join(d, "*.h"))
+                    if os.path.basename(f).startswith(kernels)):
         h.update(os.path.basename(f).encode())
         h.update(open(f, "rb").read())
     return h.hexdigest()[:16]
