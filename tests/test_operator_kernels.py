@@ -58,3 +58,21 @@ def test_wide_rows_reach_the_stores_of_any_row():
     from test_gpu_mx4_wide import WIDE
     assert all(N >= 1 << 21 and not choice(M, N, K)[2] for M, N, K in WIDE)
     assert any(N % 8 == 0 for _, N, _ in WIDE) and any(2 * N * min(M, choice(M, N, K)[0]) >= 1 << 31 for M, N, K in WIDE)
+
+
+def test_every_attention_kernel_is_reached_by_the_gpu_tests():
+    pytest.importorskip("torch")
+    from test_gpu_attention_kernels import BAD_SHAPES, CASES, DIMS
+
+    def attention_choice(*sizes):
+        out = (ctypes.c_int * 2)()
+        binding.lib().vq_internal_attention_choice(*sizes, out)
+        return out[0], out[1] > 0
+
+    for name, (kernel, divided, lq, lk, H, G) in CASES.items():
+        assert attention_choice(len(lq), sum(lq) + 5, sum(lk), H, G) == attention_choice(len(lq), sum(lq), sum(lk), H, G) == (kernel, divided), name
+        # its rows and its keys in several turns
+        assert max(lq) * H // G > (128 if kernel == 0 else 32) and max(lk) > 64 or name == "frames", name
+    assert {(c[0], c[1]) for c in CASES.values()} == {(0, False), (0, True), (1, False), (1, True), (2, False)}
+    assert {next(i for i, most in enumerate((64, 80, 96, 128)) if d <= most) for d in DIMS} == {0, 1, 2, 3}
+    assert [attention_choice(4, 100, Tk, H, G) for H, G, Tk, _, _ in BAD_SHAPES] == [s[3:] for s in BAD_SHAPES]
