@@ -4,6 +4,12 @@
 //     S = scale * Q K^T,  m' = max(m, rowmax S),  P = exp(S - m'),  l = l exp(m - m') + rowsum P,  O = O exp(m - m') + P V
 // and O / l at the end: one pass over K and V, nothing of S leaves the registers.
 //
+// m, l and O are fp32; P goes into the second product rounded to the type of V, since a matrix instruction takes one type.  Relative error
+// of fp16 outputs against 64 bits, 2.07e-4 of which is their own rounding: 2 x 4096, 16 heads of 72 2.9e-4; 2 x 16384 queries on 120 keys 2.5e-4;
+// 16 single tokens over up to 32768 keys 2.6e-4.  A second product, with what the rounding left of P, makes each of them 2.07e-4 and takes 283 us
+// instead of 207, 61 to 66 instead of 57, 175 instead of 170; 4 x 4096, 16 heads of 128 706 instead of 524, 16 x 64 rows over 4096 keys 76 to 80
+// instead of 69 (captured, inputs that are not in the caches).
+//
 // The matrix cores compute S^T = K Q^T and O^T = V^T P^T in blocks of 32 x 32 x 16: a lane's column is a query row, so that a
 // row's maximum and sum are a lane's own values and one exchange with the other half of the wavefront, and
 // the P^T that it holds after the exponentials is the operand of the second product as it lies: a lane has keys 8i + 4h + 0..3

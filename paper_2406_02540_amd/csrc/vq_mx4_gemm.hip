@@ -372,8 +372,11 @@ bool mx4_gemm_takes(int M, int N) {
 
 // The kernel for a product's sizes, by what each would take: rounds of its workgroups on the chip times a workgroup's time, fitted to
 // measurements over M 1 .. 32768, N 1152 .. 8192, K 1152 .. 8192 (us; off by 10 to 15 %).  Where the wavefronts divide K, a
-// workgroup fills a CU's LDS and takes 0.8 and 0.02 for each row of a line (256 of K), eight lines at a time; tiles of 256 x 256 take 2.0
-// a stage and 3 for their outputs, of 128 x 128, two a CU, 1.1 and 2.7, of 64 x 128 0.9 and 1.7.
+// workgroup counts as alone on its CU and takes 0.8 and 0.02 for each row of a line (256 of K), eight lines at a time; tiles of 256 x 256
+// take 2.0 a stage and 3 for their outputs, of 128 x 128, two a CU, 1.1 and 2.7, of 64 x 128 0.9 and 1.7.
+// (Tiles of 48 x 48 and 32 x 64 do fill a CU's LDS; two of 32 x 32 fit.  Counted as two with the same costs they take over up to 512 tiles:
+// 32 x 4096 -> 8224 9.0 us as it is and 10.4 so, 128 x 4096 -> 4000 9.1 and 10.0, 16 x 4096 -> 12000 9.4 and 10.1, but 96 x 4096 -> 4096 9.7 and 8.8,
+// 64 x 1152 -> 4608 5.1 and 4.4, 96 x 1152 -> 3456 5.1 and 4.6.)
 Mx4Choice choose_mx4_gemm(int M, int N, int K, int num_cus) {
     const float lines = (float)((K + 255) / 256);
     const int turns = ((int)lines + 7) / 8;

@@ -21,7 +21,8 @@ __device__ __forceinline__ void rotation(int position, float freq, float amplitu
 // A thread takes PAIRS neighbouring pairs of a token, computes their angles once and turns them in every `lanes_h`-th head, q's and
 // k's one after the other (threads behind the pairs copy as many channels that are not turned).  Neighbouring threads take
 // neighbouring pairs, then heads: a wavefront's accesses cover whole rows of a token.  Four pairs where the heads' turned part
-// divides by them, else two, else one: the second halves start at rot_dim / 2, and with them the accesses' alignment.  (36 of 72 channels, out of place, 117 us, 18 159.)
+// divides by them, else two, else one: the second halves start at rot_dim / 2, and with them the accesses' alignment.  (32768 tokens, 16 + 16 heads of 72, halves, out of place:
+// all 72 channels turned 70 us, 36 of them 117, 18 159: the bytes are the same, in accesses of 4 and 2 bytes a lane instead of 8.)
 template <class TYPE, bool INTERLEAVED, int PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a) {
     const int pieces = a.copied_from + a.copied;       // per head: four pairs, or eight channels to copy
