@@ -382,7 +382,8 @@ size_t vq_linear_mx4_workspace_bytes(int M, int N, int K);
  *   are fp32; the weights exp(score - max) are rounded to dtype for the product with v (they
  *   multiply values of that type), their sum is that of the rounded ones (72 and 80 channels) or of the fp32 ones.  Not checked on the
  *   device: k, v of a sequence finite (a value that is not reaches all of that sequence's
- *   rows), scores and softmax_scale times them within the range of fp32; cu_q, cu_k ascending and within Tq, Tk (violations give unspecified values in out, never a fault).
+ *   rows), scores and softmax_scale times them within the range of fp32; cu_q, cu_k ascending and
+ *   within Tq, Tk (violations give unspecified values in out, never a fault).
  *   head_dim % 8 == 0, at most VQ_MAX_HEAD_DIM; softmax_scale within [1e-30, 1e30].  The workspace (vq_attention_workspace_bytes, which
  *   may be 0; 16-byte aligned) holds partial results where keys are divided among workgroups;
  *   two calls that may overlap in time need one each.  Lengths lie on the device: how the work is dealt goes by the averages

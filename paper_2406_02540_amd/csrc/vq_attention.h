@@ -5,7 +5,7 @@
 // and O / l at the end: one pass over K and V, nothing of S leaves the registers.
 //
 // m, l and O are fp32; P goes into the second product rounded to the type of V, since a matrix instruction takes one type.  Relative error
-// of fp16 outputs against 64 bits, 2.07e-4 of which is their own rounding: 2 x 4096, 16 heads of 72 2.9e-4; 2 x 16384 queries on 120 keys 2.5e-4;
+// of fp16 outputs against 64 bits, where their own rounding alone makes 2.07e-4: 2 x 4096, 16 heads of 72 2.9e-4; 2 x 16384 queries on 120 keys 2.5e-4;
 // 16 single tokens over up to 32768 keys 2.6e-4.  A second product, with what the rounding left of P, makes each of them 2.07e-4 and takes 283 us
 // instead of 207, 61 to 66 instead of 57, 175 instead of 170; 4 x 4096, 16 heads of 128 706 instead of 524, 16 x 64 rows over 4096 keys 76 to 80
 // instead of 69 (captured, inputs that are not in the caches).
