@@ -403,6 +403,65 @@ int vq_attention(const void* q, const void* k, const void* v, void* out, int dty
 /* Bytes of workspace vq_attention needs for these sizes (0 too if one is invalid).  Host-only, no HIP call. */
 size_t vq_attention_workspace_bytes(int sequences, int Tq, int Tk, int heads, int kv_heads, int head_dim);
 
+/*
+ * Forms of the two operations above for images, video and serving, on the same views, with the same rules for strides,
+ * pointers, types and outputs.
+ *
+ * vq_rotary_axes: rotary positions of several axes (a token's frame, row and column, say).  Axis a turns sections[a] pairs, in
+ *   order: pair i of axis a and token t by the angle positions[a][t] * inv_freq[i], as vq_rotary does.  The channels of pair i:
+ *     VQ_PAIRS_HALVES       i and i + rot_dim/2
+ *     VQ_PAIRS_NEIGHBOURS   2i and 2i + 1
+ *     VQ_PAIRS_AXIS_HALVES  f + i and f + i + sections[a], f the pairs of the axes in front of a: each axis turns
+ *                           2 * sections[a] channels of its own, in halves
+ *   rot_dim = 2 (sections[0] + ... ), at most head_dim; channels from rot_dim on are copied.
+ *     positions  int32 [axes, T], any values
+ *     inv_freq   fp32 [rot_dim/2] (vq_rotary_frequencies of 2 * sections[a] channels for every axis, one behind the other)
+ *     sections   host, axes of them, each at least 1; axes 1 to VQ_MAX_AXES
+ *
+ * vq_norm_rotary: the norm of every head of q and k, and the rotation behind it in the same pass.
+ *     VQ_NORM_RMS    y = x / sqrt(mean x^2 + eps) * weight + bias
+ *     VQ_NORM_LAYER  y = (x - mean x) / sqrt(mean (x - mean x)^2 + eps) * weight + bias
+ *   over the head_dim channels of a head, then vq_rotary_axes of y.  All in fp32, one rounding at the end.  weight and bias are
+ *   fp32 [head_dim], those of q and those of k, each NULL for ones or zeros.  eps > 0.  axes = 0: the norm alone (positions,
+ *   inv_freq, sections, pairing and amplitude are not looked at).  Not checked on the device: the squares of a head within
+ *   the range of fp32; a head with a value that is not finite has no specified values, the others keep theirs.
+ *
+ * vq_attention_window: vq_attention in a sliding window.  With n queries and m keys query i of a sequence stands at
+ *   p = i + m - n.  It sees the keys p - left .. p + right and the sequence's first `sinks` keys, of both none behind p
+ *   if causal.  left, right: 0 or more, or -1 for no limit (right is not looked at if causal, but for its range); sinks >= 0.  A query that sees
+ *   no key gets zeros.  What a query does not see does not reach it, finite or not, but for a value of v that is not finite in a
+ *   block of 128 query rows (query heads of a head of k, then tokens) some of which see it.
+ *
+ * vq_attention_prefix: vq_attention of sequences whose first keys are the same ones, given once: every query sees all of
+ *   prefix_k, prefix_v [prefix, kv_heads, head_dim], and its own sequence's keys behind them as vq_attention has it
+ *   (causal: its keys 0 .. i + m - n).  prefix >= 0, prefix + Tk at most 2^31 - 256; a query with neither gets zeros.
+ *     strides    host, twelve of them: token and head of q, prefix_k, prefix_v, k, v, out
+ *   Few queries a sequence: the prefix is read once for all of them, and not once for every sequence.
+ */
+#define VQ_MAX_AXES 4
+typedef enum vq_pairs { VQ_PAIRS_HALVES = 0, VQ_PAIRS_NEIGHBOURS = 1, VQ_PAIRS_AXIS_HALVES = 2 } vq_pairs;
+int vq_rotary_axes(const void* q, void* q_out, const void* k, void* k_out, int dtype, const int32_t* positions,
+                   const float* inv_freq, float amplitude, int pairing, int axes, const int32_t* sections, int T, int q_heads,
+                   int k_heads, int head_dim, const int64_t* strides, void* hip_stream);
+typedef enum vq_norm { VQ_NORM_RMS = 0, VQ_NORM_LAYER = 1 } vq_norm;
+int vq_norm_rotary(const void* q, void* q_out, const void* k, void* k_out, int dtype, int norm, float eps,
+                   const float* q_weight, const float* q_bias, const float* k_weight, const float* k_bias,
+                   const int32_t* positions, const float* inv_freq, float amplitude, int pairing, int axes,
+                   const int32_t* sections, int T, int q_heads, int k_heads, int head_dim, const int64_t* strides,
+                   void* hip_stream);
+int vq_attention_window(const void* q, const void* k, const void* v, void* out, int dtype, const int32_t* cu_q,
+                        const int32_t* cu_k, int sequences, int Tq, int Tk, int heads, int kv_heads, int head_dim,
+                        const int64_t* strides, float softmax_scale, int causal, int left, int right, int sinks,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+int vq_attention_prefix(const void* q, const void* prefix_k, const void* prefix_v, const void* k, const void* v, void* out,
+                        int dtype, const int32_t* cu_q, const int32_t* cu_k, int sequences, int Tq, int prefix, int Tk,
+                        int heads, int kv_heads, int head_dim, const int64_t* strides, float softmax_scale, int causal,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Bytes of workspace they need for these sizes (0 too if one is invalid).  Host-only, no HIP call. */
+size_t vq_attention_window_workspace_bytes(int sequences, int Tq, int Tk, int heads, int kv_heads, int head_dim, int causal,
+                                           int left, int right, int sinks);
+size_t vq_attention_prefix_workspace_bytes(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim);
+
 /* Static, host-side description of a vq_status value (no passage of the paper: the error
  * reporting of this boundary). */
 const char* vq_status_string(int status);

@@ -58,6 +58,12 @@ SIGNATURES = {
     "vq_rotary_frequencies": (_I, [_P, _P, _I, _D, _I, _D, _I]),
     "vq_attention": (_I, [_P, _P, _P, _P, _I, _P, _P, _I, _I, _I, _I, _I, _I, _P, _F, _I, _P, _SZ, _P]),
     "vq_attention_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I, _I]),
+    "vq_rotary_axes": (_I, [_P, _P, _P, _P, _I, _P, _P, _F, _I, _I, _P, _I, _I, _I, _I, _P, _P]),
+    "vq_norm_rotary": (_I, [_P, _P, _P, _P, _I, _I, _F, _P, _P, _P, _P, _P, _P, _F, _I, _I, _P, _I, _I, _I, _I, _P, _P]),
+    "vq_attention_window": (_I, [_P, _P, _P, _P, _I, _P, _P, _I, _I, _I, _I, _I, _I, _P, _F, _I, _I, _I, _I, _P, _SZ, _P]),
+    "vq_attention_prefix": (_I, [_P, _P, _P, _P, _P, _P, _I, _P, _P, _I, _I, _I, _I, _I, _I, _I, _P, _F, _I, _P, _SZ, _P]),
+    "vq_attention_window_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I, _I, _I, _I, _I, _I]),
+    "vq_attention_prefix_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I, _I, _I]),
     "vq_status_string": (ctypes.c_char_p, [_I]),
 }
 
@@ -97,7 +103,8 @@ _BOUND = ("vq_quantize_per_token", "vq_gelu_quantize", "vq_layernorm_quantize", 
           "vq_quantize_weight", "vq_gemm_f16", "vq_gemm_w8a8", "vq_gemm_w4a8", "vq_linear_workspace_bytes", "vq_linear",
           "vq_linear_static", "vq_layernorm_linear", "vq_gelu_linear", "vq_residual_linear", "vq_hadamard_linear",
           "vq_mx4_quantize", "vq_mx4_dequantize", "vq_gemm_mx4", "vq_linear_mx4", "vq_linear_mx4_workspace_bytes",
-          "vq_rotary", "vq_attention", "vq_attention_workspace_bytes")
+          "vq_rotary", "vq_attention", "vq_attention_workspace_bytes", "vq_rotary_axes", "vq_norm_rotary", "vq_attention_window",
+          "vq_attention_prefix", "vq_attention_window_workspace_bytes", "vq_attention_prefix_workspace_bytes")
 
 _ext = None
 
@@ -295,3 +302,56 @@ def vq_attention(q, k, v, cu_q, cu_k, softmax_scale=None, causal=False, out=None
     cu[b] and cu[b+1] (int32 [sequences + 1]) -> out [Tq,H,D].  softmax_scale: 1/sqrt(D) if not given; workspace is a
     uint8 device tensor (allocated if None).  Rows outside all sequences are not written (a new out is not cleared)."""
     return (_ext or _load()).attention(q, k, v, cu_q, cu_k, softmax_scale, causal, out, workspace, stream)
+
+
+ROPE_PAIRS = {"halves": 0, "neighbours": 1, "axis_halves": 2}
+NORMS = {"rms": 0, "layer": 1}
+
+
+def _named(table, name, what):
+    if name not in table:
+        raise ValueError(f"{what} must be one of {tuple(table)}")
+    return table[name]
+
+
+def vq_rotary_axes(q, k, positions, inv_freq, sections, pairing="halves", amplitude=1.0, q_out=None, k_out=None, stream=None):
+    """Rotary positions of several axes on views q [T,Hq,D] and k [T,Hk,D] (or None), fp16 or bf16: axis a turns sections[a]
+    pairs by positions[a] (int32 [axes,T]) times their part of inv_freq fp32 [sum(sections)]; pairing "halves" (over all axes),
+    "neighbours" or "axis_halves" (every axis in channels of its own) -> (q_out, k_out); q_out=q, k_out=k works in place."""
+    return (_ext or _load()).rotary_axes(q, k, positions, inv_freq, sections, _named(ROPE_PAIRS, pairing, "pairing"), amplitude, q_out,
+                                         k_out, stream)
+
+
+def vq_norm_rotary(q, k, q_weight=None, k_weight=None, q_bias=None, k_bias=None, norm="rms", eps=1e-6, positions=None, inv_freq=None,
+                   sections=None, pairing="halves", amplitude=1.0, q_out=None, k_out=None, stream=None):
+    """The norm of every head of q and k ("rms", or "layer": mean and variance), weights and biases fp32 [D] or None, and the
+    rotary positions of vq_rotary_axes behind it in the same pass (sections=None: the norm alone) -> (q_out, k_out)."""
+    return (_ext or _load()).norm_rotary(q, k, q_weight, k_weight, q_bias, k_bias, _named(NORMS, norm, "norm"), eps, positions, inv_freq,
+                                         sections, _named(ROPE_PAIRS, pairing, "pairing"), amplitude, q_out, k_out, stream)
+
+
+def _limit(n):
+    return -1 if n is None else int(n)
+
+
+def vq_attention_window_workspace_bytes(sequences, Tq, Tk, heads, kv_heads, head_dim, causal, left, right, sinks) -> int:
+    return int(lib().vq_attention_window_workspace_bytes(int(sequences), int(Tq), int(Tk), int(heads), int(kv_heads), int(head_dim),
+                                                         int(causal), _limit(left), _limit(right), int(sinks)))
+
+
+def vq_attention_window(q, k, v, cu_q, cu_k, left, right=None, sinks=0, softmax_scale=None, causal=False, out=None, workspace=None,
+                        stream=None):
+    """vq_attention in a sliding window: of n queries and m keys query i, at p = i + m - n, sees the keys p - left .. p + right
+    (None: no limit) and the first `sinks`; causal: none behind p.  Other arguments as vq_attention's."""
+    return (_ext or _load()).attention_window(q, k, v, cu_q, cu_k, left, right, sinks, softmax_scale, causal, out, workspace, stream)
+
+
+def vq_attention_prefix_workspace_bytes(sequences, Tq, prefix, Tk, heads, kv_heads, head_dim) -> int:
+    return int(lib().vq_attention_prefix_workspace_bytes(int(sequences), int(Tq), int(prefix), int(Tk), int(heads), int(kv_heads),
+                                                         int(head_dim)))
+
+
+def vq_attention_prefix(q, prefix_k, prefix_v, k, v, cu_q, cu_k, softmax_scale=None, causal=False, out=None, workspace=None, stream=None):
+    """vq_attention of sequences that share their first keys prefix_k, prefix_v [P,G,D]: a query sees all of them, then its own
+    sequence's keys (causal: up to its place).  Other arguments as vq_attention's."""
+    return (_ext or _load()).attention_prefix(q, prefix_k, prefix_v, k, v, cu_q, cu_k, softmax_scale, causal, out, workspace, stream)

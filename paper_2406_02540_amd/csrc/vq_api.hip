@@ -2,6 +2,7 @@
 // Declarations and the contract of every entry point are in include/vq.h.
 #include <atomic>
 #include <cmath>
+#include <initializer_list>
 
 #include "vq.h"
 #include "vq_internal.h"
@@ -256,6 +257,92 @@ bool strides_ok(const int64_t* s, int tokens, int heads, int head_dim, bool writ
 }
 constexpr int64_t kMaxKeyStride = 1 << 23;   // a tile's offsets are 32-bit
 constexpr int kMaxRows = 0x7FFFFF00;         // rows and keys of a last tile fit an int
+
+bool rotary_sizes_ok(int T, int q_heads, int k_heads, int head_dim) {
+    return T >= 0 && q_heads > 0 && k_heads >= 0 && q_heads <= 1 << 16 && k_heads <= 1 << 16 && head_dim > 0 && head_dim % 8 == 0 &&
+           head_dim <= VQ_MAX_HEAD_DIM;
+}
+int validate_rotary_views(const void* q, const void* q_out, const void* k, const void* k_out, int T, int q_heads, int k_heads, int head_dim,
+                          const int64_t* strides) {
+    if (!q || !q_out || (k_heads > 0 && (!k || !k_out)) || !strides) return VQ_ERR_NULL;
+    for (int i = 0; i < (k_heads > 0 ? 4 : 2); ++i)
+        if (!strides_ok(strides + 2 * i, T, i < 2 ? q_heads : k_heads, head_dim, i % 2 == 1)) return VQ_ERR_SHAPE;
+    if (q == q_out && (strides[0] != strides[2] || strides[1] != strides[3])) return VQ_ERR_SHAPE;
+    if (k_heads > 0 && k == k_out && (strides[4] != strides[6] || strides[5] != strides[7])) return VQ_ERR_SHAPE;
+    if (misaligned(q) || misaligned(q_out) || (k_heads > 0 && (misaligned(k) || misaligned(k_out)))) return VQ_ERR_ALIGN;
+    return VQ_OK;
+}
+template <class ARGS>
+void set_views(ARGS& a, const void* q, void* q_out, const void* k, void* k_out, int T, int q_heads, int k_heads, int head_dim, const int64_t* strides) {
+    a.q = q, a.q_out = q_out, a.T = T, a.q_heads = q_heads, a.k_heads = k_heads, a.head_dim = head_dim;
+    a.q_token = strides[0], a.q_head = strides[1], a.qo_token = strides[2], a.qo_head = strides[3];
+    if (k_heads > 0) {
+        a.k = k, a.k_out = k_out;
+        a.k_token = strides[4], a.k_head = strides[5], a.ko_token = strides[6], a.ko_head = strides[7];
+    }
+}
+
+// The axes of a rotation; the pairs of all of them, or 0 if they are none that the calls take.
+int pairs_of(int pairing, int axes, const int32_t* sections, int head_dim) {
+    if (pairing < VQ_PAIRS_HALVES || pairing > VQ_PAIRS_AXIS_HALVES || axes < 1 || axes > VQ_MAX_AXES) return 0;
+    int64_t pairs = 0;
+    for (int i = 0; i < axes; ++i) {
+        if (sections[i] < 1) return 0;
+        pairs += sections[i];
+    }
+    return 2 * pairs <= head_dim ? (int)pairs : 0;
+}
+
+// ---- attention's arguments -----------------------------------------------------------------------------------
+
+bool attention_sizes_ok(int sequences, int Tq, int64_t Tk, int heads, int kv_heads, int head_dim) {
+    return sequences >= 0 && Tq >= 0 && Tk >= 0 && heads > 0 && kv_heads > 0 && heads <= 1 << 16 && heads % kv_heads == 0 &&
+           (int64_t)Tq * heads <= kMaxRows && Tk <= kMaxRows && head_dim > 0 && head_dim % 8 == 0 && head_dim <= VQ_MAX_HEAD_DIM;
+}
+bool attention_scale_ok(float softmax_scale) { return softmax_scale >= 1e-30f && softmax_scale <= 1e30f; }
+// The views of a call: queries, keys and values (not looked at where there are no tokens), and what is written.
+struct View {
+    const void* p;
+    const int64_t* strides;
+    int tokens, heads;
+    enum { kQueries, kKeys, kOutput } role;
+};
+int validate_views(std::initializer_list<View> views, const int32_t* cu_q, const int32_t* cu_k, int head_dim) {
+    if (!cu_q || !cu_k) return VQ_ERR_NULL;
+    for (const View& v : views)
+        if (!v.p && (v.role != View::kKeys || v.tokens > 0)) return VQ_ERR_NULL;
+    for (const View& v : views) {
+        if (!strides_ok(v.strides, v.tokens, v.heads, head_dim, v.role == View::kOutput)) return VQ_ERR_SHAPE;
+        if (v.role == View::kKeys && v.strides[0] > kMaxKeyStride) return VQ_ERR_SHAPE;
+    }
+    for (const View& v : views)
+        if (misaligned(v.p) && (v.role != View::kKeys || v.tokens > 0)) return VQ_ERR_ALIGN;
+    return misaligned4(cu_q) || misaligned4(cu_k) ? VQ_ERR_ALIGN : VQ_OK;
+}
+int validate_workspace(const void* workspace, size_t bytes, size_t need) {
+    if (need == 0) return VQ_OK;
+    if (!workspace) return VQ_ERR_NULL;
+    if (misaligned(workspace)) return VQ_ERR_ALIGN;
+    return bytes < need ? VQ_ERR_WORKSPACE : VQ_OK;
+}
+bool window_ok(int causal, int left, int right, int sinks) { return (causal == 0 || causal == 1) && left >= -1 && right >= -1 && sinks >= 0; }
+// Partial sums, maxima and weights of a call whose keys are divided.
+size_t workspace_of(const vq::AttentionChoice& choice, int Tq, int heads, int head_dim) {
+    const size_t parts = (size_t)1 << choice.split_shift;
+    return parts == 1 || !choice.fits ? 0 : parts * (size_t)Tq * (size_t)heads * (size_t)(head_dim + 2) * sizeof(float);
+}
+// strides: token and head of q, k, v, out.
+template <class ARGS>
+void set_attention(ARGS& a, const void* q, const void* k, const void* v, void* out, const int32_t* cu_q, const int32_t* cu_k, int sequences, int Tq, int Tk,
+                   int heads, int kv_heads, int head_dim, const int64_t* strides, float softmax_scale, int causal) {
+    a.q = q, a.k = k, a.v = v, a.out = out, a.cu_q = cu_q, a.cu_k = cu_k;
+    a.sequences = sequences, a.Tq = Tq, a.Tk = Tk, a.heads = heads, a.kv_heads = kv_heads, a.group = heads / kv_heads;
+    a.head_dim = head_dim, a.causal = causal;
+    a.q_token = strides[0], a.q_head = strides[1], a.k_token = strides[2], a.k_head = strides[3];
+    a.v_token = strides[4], a.v_head = strides[5], a.o_token = strides[6], a.o_head = strides[7];
+    a.scale_log2 = (float)((double)softmax_scale * 1.44269504088896340736);
+    a.group_shift = (a.group & (a.group - 1)) == 0 ? __builtin_ctz(a.group) : -1;
+}
 
 }  // namespace
 
@@ -556,29 +643,19 @@ int vq_rotary(const void* q, void* q_out, const void* k, void* k_out, int dtype,
               const float* inv_freq, float amplitude, int interleaved, int T, int q_heads, int k_heads, int head_dim,
               int rot_dim, const int64_t* strides, void* hip_stream) {
     if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
-    if (T < 0 || q_heads <= 0 || k_heads < 0 || q_heads > 1 << 16 || k_heads > 1 << 16 || head_dim <= 0 || head_dim % 8 != 0 ||
-        head_dim > VQ_MAX_HEAD_DIM || rot_dim <= 0 || rot_dim % 2 != 0 || rot_dim > head_dim ||
+    if (!rotary_sizes_ok(T, q_heads, k_heads, head_dim) || rot_dim <= 0 || rot_dim % 2 != 0 || rot_dim > head_dim ||
         (interleaved != 0 && interleaved != 1) || !std::isfinite(amplitude))
         return VQ_ERR_SHAPE;
     if (T == 0) return VQ_OK;
-    if (!q || !q_out || (k_heads > 0 && (!k || !k_out)) || !positions || !inv_freq || !strides) return VQ_ERR_NULL;
-    for (int i = 0; i < (k_heads > 0 ? 4 : 2); ++i)
-        if (!strides_ok(strides + 2 * i, T, i < 2 ? q_heads : k_heads, head_dim, i % 2 == 1)) return VQ_ERR_SHAPE;
-    if (q == q_out && (strides[0] != strides[2] || strides[1] != strides[3])) return VQ_ERR_SHAPE;
-    if (k_heads > 0 && k == k_out && (strides[4] != strides[6] || strides[5] != strides[7])) return VQ_ERR_SHAPE;
-    if (misaligned(q) || misaligned(q_out) || misaligned(inv_freq) || misaligned4(positions) ||
-        (k_heads > 0 && (misaligned(k) || misaligned(k_out))))
-        return VQ_ERR_ALIGN;
+    if (!positions || !inv_freq) return VQ_ERR_NULL;
+    const int v = validate_rotary_views(q, q_out, k, k_out, T, q_heads, k_heads, head_dim, strides);
+    if (v != VQ_OK) return v;
+    if (misaligned(inv_freq) || misaligned4(positions)) return VQ_ERR_ALIGN;
     const int arch = check_arch();
     if (arch != VQ_OK) return arch;
     vq::RotaryArgs a{};
-    a.q = q, a.q_out = q_out, a.positions = positions, a.inv_freq = inv_freq, a.amplitude = amplitude;
-    a.T = T, a.q_heads = q_heads, a.k_heads = k_heads, a.head_dim = head_dim, a.rot_dim = rot_dim;
-    a.q_token = strides[0], a.q_head = strides[1], a.qo_token = strides[2], a.qo_head = strides[3];
-    if (k_heads > 0) {
-        a.k = k, a.k_out = k_out;
-        a.k_token = strides[4], a.k_head = strides[5], a.ko_token = strides[6], a.ko_head = strides[7];
-    }
+    set_views(a, q, q_out, k, k_out, T, q_heads, k_heads, head_dim, strides);
+    a.positions = positions, a.inv_freq = inv_freq, a.amplitude = amplitude, a.rot_dim = rot_dim;
     return launch_status(vq::launch_rotary(a, dtype, interleaved, (hipStream_t)hip_stream));
 }
 
@@ -610,54 +687,145 @@ int vq_rotary_frequencies(float* inv_freq, float* amplitude, int rot_dim, double
 }
 
 size_t vq_attention_workspace_bytes(int sequences, int Tq, int Tk, int heads, int kv_heads, int head_dim) {
-    if (sequences <= 0 || Tq <= 0 || Tk < 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0 || head_dim <= 0 ||
-        head_dim % 8 != 0 || head_dim > VQ_MAX_HEAD_DIM)
-        return 0;
-    if ((int64_t)Tq * heads > kMaxRows || Tk > kMaxRows) return 0;
-    const vq::AttentionChoice choice = vq::choose_attention(sequences, Tq, Tk, heads, kv_heads);
-    const size_t parts = (size_t)1 << choice.split_shift;
-    return parts == 1 || !choice.fits ? 0 : parts * (size_t)Tq * (size_t)heads * (size_t)(head_dim + 2) * sizeof(float);
+    if (!attention_sizes_ok(sequences, Tq, Tk, heads, kv_heads, head_dim) || sequences == 0 || Tq == 0) return 0;
+    return workspace_of(vq::choose_attention(sequences, Tq, Tk, heads, kv_heads), Tq, heads, head_dim);
 }
 
 int vq_attention(const void* q, const void* k, const void* v, void* out, int dtype, const int32_t* cu_q, const int32_t* cu_k,
                  int sequences, int Tq, int Tk, int heads, int kv_heads, int head_dim, const int64_t* strides,
                  float softmax_scale, int causal, void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
-    if (sequences < 0 || Tq < 0 || Tk < 0 || heads <= 0 || kv_heads <= 0 || heads > 1 << 16 || heads % kv_heads != 0 ||
-        (int64_t)Tq * heads > kMaxRows || Tk > kMaxRows || head_dim <= 0 || head_dim % 8 != 0 || head_dim > VQ_MAX_HEAD_DIM || (causal != 0 && causal != 1) ||
-        !(softmax_scale >= 1e-30f && softmax_scale <= 1e30f))
+    if (!attention_sizes_ok(sequences, Tq, Tk, heads, kv_heads, head_dim) || (causal != 0 && causal != 1) || !attention_scale_ok(softmax_scale))
         return VQ_ERR_SHAPE;
     if (sequences == 0 || Tq == 0) return VQ_OK;
     const vq::AttentionChoice choice = vq::choose_attention(sequences, Tq, Tk, heads, kv_heads);
     if (!choice.fits) return VQ_ERR_SHAPE;
-    if (!q || !out || !cu_q || !cu_k || !strides || (Tk > 0 && (!k || !v))) return VQ_ERR_NULL;
-    for (int i = 0; i < 4; ++i) {
-        const bool keys = i == 1 || i == 2;
-        if (!strides_ok(strides + 2 * i, keys ? Tk : Tq, keys ? kv_heads : heads, head_dim, i == 3)) return VQ_ERR_SHAPE;
-        if (keys && strides[2 * i] > kMaxKeyStride) return VQ_ERR_SHAPE;
-    }
-    if (misaligned(q) || misaligned(out) || (Tk > 0 && (misaligned(k) || misaligned(v))) || misaligned4(cu_q) || misaligned4(cu_k))
-        return VQ_ERR_ALIGN;
-    const size_t need = vq_attention_workspace_bytes(sequences, Tq, Tk, heads, kv_heads, head_dim);
-    if (need > 0) {
-        if (!workspace) return VQ_ERR_NULL;
-        if (misaligned(workspace)) return VQ_ERR_ALIGN;
-        if (workspace_bytes < need) return VQ_ERR_WORKSPACE;
-    }
-    const int arch = check_arch();
-    if (arch != VQ_OK) return arch;
+    if (!strides) return VQ_ERR_NULL;
+    int status = validate_views({{q, strides, Tq, heads, View::kQueries}, {k, strides + 2, Tk, kv_heads, View::kKeys},
+                                 {v, strides + 4, Tk, kv_heads, View::kKeys}, {out, strides + 6, Tq, heads, View::kOutput}}, cu_q, cu_k, head_dim);
+    if (status == VQ_OK) status = validate_workspace(workspace, workspace_bytes, vq_attention_workspace_bytes(sequences, Tq, Tk, heads, kv_heads, head_dim));
+    if (status == VQ_OK) status = check_arch();
+    if (status != VQ_OK) return status;
     vq::AttentionArgs a{};
-    a.q = q, a.k = k, a.v = v, a.out = out, a.cu_q = cu_q, a.cu_k = cu_k;
-    a.sequences = sequences, a.Tq = Tq, a.Tk = Tk, a.heads = heads, a.kv_heads = kv_heads, a.group = heads / kv_heads;
-    a.head_dim = head_dim, a.causal = causal;
-    a.q_token = strides[0], a.q_head = strides[1], a.k_token = strides[2], a.k_head = strides[3];
-    a.v_token = strides[4], a.v_head = strides[5], a.o_token = strides[6], a.o_head = strides[7];
-    a.scale_log2 = (float)((double)softmax_scale * 1.44269504088896340736);
-    a.group_shift = (a.group & (a.group - 1)) == 0 ? __builtin_ctz(a.group) : -1;
+    set_attention(a, q, k, v, out, cu_q, cu_k, sequences, Tq, Tk, heads, kv_heads, head_dim, strides, softmax_scale, causal);
     a.split_shift = choice.split_shift;
     a.part_o = (float*)workspace;
     a.part_ml = a.part_o ? a.part_o + ((size_t)Tq << a.split_shift) * heads * head_dim : nullptr;
     return launch_status(vq::launch_attention(a, choice.kernel, dtype, (hipStream_t)hip_stream));
+}
+
+int vq_rotary_axes(const void* q, void* q_out, const void* k, void* k_out, int dtype, const int32_t* positions,
+                   const float* inv_freq, float amplitude, int pairing, int axes, const int32_t* sections, int T, int q_heads,
+                   int k_heads, int head_dim, const int64_t* strides, void* hip_stream) {
+    if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
+    if (!rotary_sizes_ok(T, q_heads, k_heads, head_dim) || !std::isfinite(amplitude)) return VQ_ERR_SHAPE;
+    if (!sections) return VQ_ERR_NULL;
+    const int pairs = pairs_of(pairing, axes, sections, head_dim);
+    if (pairs == 0) return VQ_ERR_SHAPE;
+    if (T == 0) return VQ_OK;
+    if (!positions || !inv_freq) return VQ_ERR_NULL;
+    int status = validate_rotary_views(q, q_out, k, k_out, T, q_heads, k_heads, head_dim, strides);
+    if (status == VQ_OK && (misaligned(inv_freq) || misaligned4(positions))) status = VQ_ERR_ALIGN;
+    if (status == VQ_OK) status = check_arch();
+    if (status != VQ_OK) return status;
+    vq::RotaryAxesArgs a{};
+    set_views(a, q, q_out, k, k_out, T, q_heads, k_heads, head_dim, strides);
+    a.positions = positions, a.inv_freq = inv_freq, a.amplitude = amplitude, a.pairing = pairing, a.axes = axes, a.pairs = pairs;
+    for (int i = 0; i < axes; ++i) a.sections[i] = sections[i];
+    return launch_status(vq::launch_rotary_axes(a, dtype, (hipStream_t)hip_stream));
+}
+
+int vq_norm_rotary(const void* q, void* q_out, const void* k, void* k_out, int dtype, int norm, float eps,
+                   const float* q_weight, const float* q_bias, const float* k_weight, const float* k_bias,
+                   const int32_t* positions, const float* inv_freq, float amplitude, int pairing, int axes,
+                   const int32_t* sections, int T, int q_heads, int k_heads, int head_dim, const int64_t* strides,
+                   void* hip_stream) {
+    if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
+    if (!rotary_sizes_ok(T, q_heads, k_heads, head_dim) || (norm != VQ_NORM_RMS && norm != VQ_NORM_LAYER) || !(eps > 0.0f) || !std::isfinite(eps) ||
+        axes < 0 || (axes > 0 && !std::isfinite(amplitude)))
+        return VQ_ERR_SHAPE;
+    int pairs = 0;
+    if (axes > 0) {
+        if (!sections) return VQ_ERR_NULL;
+        pairs = pairs_of(pairing, axes, sections, head_dim);
+        if (pairs == 0) return VQ_ERR_SHAPE;
+    }
+    if (T == 0) return VQ_OK;
+    if (axes > 0 && (!positions || !inv_freq)) return VQ_ERR_NULL;
+    int status = validate_rotary_views(q, q_out, k, k_out, T, q_heads, k_heads, head_dim, strides);
+    if (status == VQ_OK && axes > 0 && (misaligned(inv_freq) || misaligned4(positions))) status = VQ_ERR_ALIGN;
+    for (const float* v : {q_weight, q_bias, k_heads > 0 ? k_weight : nullptr, k_heads > 0 ? k_bias : nullptr})
+        if (status == VQ_OK && v && misaligned(v)) status = VQ_ERR_ALIGN;
+    if (status == VQ_OK) status = check_arch();
+    if (status != VQ_OK) return status;
+    vq::RotaryAxesArgs a{};
+    set_views(a, q, q_out, k, k_out, T, q_heads, k_heads, head_dim, strides);
+    a.norm = 1 + norm, a.eps = eps;
+    a.weight[0] = q_weight, a.weight[1] = k_weight, a.bias[0] = q_bias, a.bias[1] = k_bias;
+    if (axes > 0) {
+        a.positions = positions, a.inv_freq = inv_freq, a.amplitude = amplitude, a.pairing = pairing, a.axes = axes, a.pairs = pairs;
+        for (int i = 0; i < axes; ++i) a.sections[i] = sections[i];
+    }
+    return launch_status(vq::launch_rotary_axes(a, dtype, (hipStream_t)hip_stream));
+}
+
+size_t vq_attention_window_workspace_bytes(int sequences, int Tq, int Tk, int heads, int kv_heads, int head_dim, int causal, int left, int right,
+                                           int sinks) {
+    if (!attention_sizes_ok(sequences, Tq, Tk, heads, kv_heads, head_dim) || sequences == 0 || Tq == 0 || !window_ok(causal, left, right, sinks)) return 0;
+    return workspace_of(vq::choose_attention_window(sequences, Tq, Tk, heads, kv_heads, causal, left, right, sinks), Tq, heads, head_dim);
+}
+
+int vq_attention_window(const void* q, const void* k, const void* v, void* out, int dtype, const int32_t* cu_q, const int32_t* cu_k, int sequences,
+                        int Tq, int Tk, int heads, int kv_heads, int head_dim, const int64_t* strides, float softmax_scale, int causal, int left,
+                        int right, int sinks, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
+    if (!attention_sizes_ok(sequences, Tq, Tk, heads, kv_heads, head_dim) || !window_ok(causal, left, right, sinks) || !attention_scale_ok(softmax_scale))
+        return VQ_ERR_SHAPE;
+    if (sequences == 0 || Tq == 0) return VQ_OK;
+    const vq::AttentionChoice choice = vq::choose_attention_window(sequences, Tq, Tk, heads, kv_heads, causal, left, right, sinks);
+    if (!choice.fits) return VQ_ERR_SHAPE;
+    if (!strides) return VQ_ERR_NULL;
+    int status = validate_views({{q, strides, Tq, heads, View::kQueries}, {k, strides + 2, Tk, kv_heads, View::kKeys},
+                                 {v, strides + 4, Tk, kv_heads, View::kKeys}, {out, strides + 6, Tq, heads, View::kOutput}}, cu_q, cu_k, head_dim);
+    if (status == VQ_OK) status = validate_workspace(workspace, workspace_bytes, workspace_of(choice, Tq, heads, head_dim));
+    if (status == VQ_OK) status = check_arch();
+    if (status != VQ_OK) return status;
+    vq::AttentionWindowArgs a{};
+    set_attention(a, q, k, v, out, cu_q, cu_k, sequences, Tq, Tk, heads, kv_heads, head_dim, strides, softmax_scale, causal);
+    // (no query stands behind Tk - 1; those that look ahead may stand far in front of 0)
+    a.left = left < 0 || left > Tk ? Tk : left, a.right = causal ? 0 : right, a.sinks = sinks < Tk ? sinks : Tk;
+    a.split_shift = choice.split_shift;
+    a.part_o = (float*)workspace;
+    a.part_ml = a.part_o ? a.part_o + ((size_t)Tq << a.split_shift) * heads * head_dim : nullptr;
+    return launch_status(vq::launch_attention_window(a, choice.kernel, dtype, (hipStream_t)hip_stream));
+}
+
+size_t vq_attention_prefix_workspace_bytes(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim) {
+    if (prefix < 0 || Tk < 0 || !attention_sizes_ok(sequences, Tq, (int64_t)prefix + Tk, heads, kv_heads, head_dim) || sequences == 0 || Tq == 0) return 0;
+    return 0;
+}
+
+int vq_attention_prefix(const void* q, const void* prefix_k, const void* prefix_v, const void* k, const void* v, void* out, int dtype,
+                        const int32_t* cu_q, const int32_t* cu_k, int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim,
+                        const int64_t* strides, float softmax_scale, int causal, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
+    if (prefix < 0 || Tk < 0 || !attention_sizes_ok(sequences, Tq, (int64_t)prefix + Tk, heads, kv_heads, head_dim) || (causal != 0 && causal != 1) ||
+        !attention_scale_ok(softmax_scale))
+        return VQ_ERR_SHAPE;
+    if (sequences == 0 || Tq == 0) return VQ_OK;
+    if (!strides) return VQ_ERR_NULL;
+    int status = validate_views({{q, strides, Tq, heads, View::kQueries}, {prefix_k, strides + 2, prefix, kv_heads, View::kKeys},
+                                 {prefix_v, strides + 4, prefix, kv_heads, View::kKeys}, {k, strides + 6, Tk, kv_heads, View::kKeys},
+                                 {v, strides + 8, Tk, kv_heads, View::kKeys}, {out, strides + 10, Tq, heads, View::kOutput}}, cu_q, cu_k, head_dim);
+    if (status == VQ_OK) status = validate_workspace(workspace, workspace_bytes, vq_attention_prefix_workspace_bytes(sequences, Tq, prefix, Tk, heads, kv_heads, head_dim));
+    if (status == VQ_OK) status = check_arch();
+    if (status != VQ_OK) return status;
+    const int64_t own[8] = {strides[0], strides[1], strides[6], strides[7], strides[8], strides[9], strides[10], strides[11]};
+    vq::AttentionPrefixArgs a{};
+    set_attention(a, q, k, v, out, cu_q, cu_k, sequences, Tq, Tk, heads, kv_heads, head_dim, own, softmax_scale, causal);
+    a.prefix_k = prefix_k, a.prefix_v = prefix_v, a.prefix = prefix;
+    a.pk_token = strides[2], a.pk_head = strides[3], a.pv_token = strides[4], a.pv_head = strides[5];
+    return launch_status(vq::launch_attention_prefix(a, dtype, (hipStream_t)hip_stream));
 }
 
 const char* vq_status_string(int status) {

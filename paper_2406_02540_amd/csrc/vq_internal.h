@@ -118,6 +118,24 @@ struct RotaryArgs {
 };
 hipError_t launch_rotary(RotaryArgs a, int dtype, int interleaved, hipStream_t stream);
 
+// Rotary positions of several axes, and the norm in front of them (vq_rotary_axes.hip).
+struct RotaryAxesArgs {
+    const void* q;
+    void* q_out;
+    const void* k;
+    void* k_out;
+    const int32_t* positions;     // [axes, T]
+    const float* inv_freq;        // [pairs]
+    const float* weight[2];       // of q and of k, or null
+    const float* bias[2];
+    float amplitude, eps;
+    int norm;                     // 0: none, else 1 + vq_norm
+    int pairing, axes, pairs, sections[VQ_MAX_AXES];
+    int T, q_heads, k_heads, head_dim;
+    int64_t q_token, q_head, qo_token, qo_head, k_token, k_head, ko_token, ko_head;   // strides in elements
+};
+hipError_t launch_rotary_axes(RotaryAxesArgs a, int dtype, hipStream_t stream);
+
 struct AttentionArgs {
     const void* q;
     const void* k;
@@ -150,6 +168,22 @@ hipError_t launch_attention(const AttentionArgs& a, AttentionKernel kernel, int 
 constexpr int kTileRows = 128;
 inline long attention_items(int sequences, int Tq, int group) { return (long)Tq * group / kTileRows + sequences; }
 hipError_t launch_attention_tiles(const AttentionArgs& a, int dtype, hipStream_t stream);
+
+// Attention in a sliding window (vq_attention_window.hip): keys p - left .. p + right (right < 0: no limit) and the first sinks.
+struct AttentionWindowArgs : AttentionArgs {
+    int left, right, sinks;
+};
+AttentionChoice choose_attention_window(int sequences, int Tq, int Tk, int heads, int kv_heads, int causal, int left, int right, int sinks);
+hipError_t launch_attention_window(const AttentionWindowArgs& a, AttentionKernel kernel, int dtype, hipStream_t stream);
+
+// Attention behind keys that all sequences share (vq_attention_prefix.hip).
+struct AttentionPrefixArgs : AttentionArgs {
+    const void* prefix_k;
+    const void* prefix_v;
+    int prefix;
+    int64_t pk_token, pk_head, pv_token, pv_head;
+};
+hipError_t launch_attention_prefix(const AttentionPrefixArgs& a, int dtype, hipStream_t stream);
 
 }  // namespace vq
 

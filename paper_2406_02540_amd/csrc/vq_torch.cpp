@@ -67,6 +67,12 @@ struct Entries {
     decltype(&::vq_rotary) rotary;
     decltype(&::vq_attention) attention;
     decltype(&::vq_attention_workspace_bytes) attention_workspace_bytes;
+    decltype(&::vq_rotary_axes) rotary_axes;
+    decltype(&::vq_norm_rotary) norm_rotary;
+    decltype(&::vq_attention_window) attention_window;
+    decltype(&::vq_attention_prefix) attention_prefix;
+    decltype(&::vq_attention_window_workspace_bytes) attention_window_workspace_bytes;
+    decltype(&::vq_attention_prefix_workspace_bytes) attention_prefix_workspace_bytes;
 } g_lib;
 static_assert(sizeof(Entries) % sizeof(void*) == 0, "a plain array of addresses");
 constexpr Py_ssize_t kEntries = sizeof(Entries) / sizeof(void*);
@@ -876,6 +882,203 @@ PyObject* attention(PyObject* const* a) {  // q k v cu_q cu_k softmax_scale caus
     return out.release();
 }
 
+// A whole number that fits the library's int (what does not is VQ_ERR_SHAPE: narrowed, it would be another); None gives `none`.
+int whole(PyObject* o, int none, const char* where) {
+    if (o == Py_None) return none;
+    PyObject* l = PyNumber_Index(o);
+    if (!l) throw Raised{};
+    int overflow = 0;
+    const long v = PyLong_AsLongAndOverflow(l, &overflow);
+    Py_DECREF(l);
+    if (v == -1 && PyErr_Occurred()) throw Raised{};
+    if (overflow || v < INT_MIN || v > INT_MAX) raise_status(VQ_ERR_SHAPE, where);
+    return (int)v;
+}
+
+// What the two calls with axes share: views of q and k, their outputs, positions [axes, T] of the pairs of every axis.
+struct AxesCall {
+    const at::Tensor& first;
+    const int code;
+    const OnDevice device;
+    const CallStream st;
+    const Heads q;
+    const bool has_k;
+    const Heads k;
+    int T, hq, hk, D, axes = 0;
+    int32_t sections[VQ_MAX_AXES] = {};
+    const at::Tensor* positions = nullptr;
+    const at::Tensor* freq = nullptr;
+    HeadsOutput qo, ko;
+    int64_t strides[8];
+    AxesCall(PyObject* q_o, PyObject* k_o, PyObject* stream, const char* where)
+        : first(some_device_tensor(q_o, "q")), code(type_code(first.scalar_type(), false, "q")), device(first), st(stream), q(first, "q"),
+          has_k(k_o != Py_None), k(has_k ? heads_argument(k_o, first.scalar_type(), "k") : q) {
+        if (k.tokens != q.tokens || k.channels != q.channels) fail(PyExc_ValueError, "k must have q's tokens and channels");
+        T = fits_int(q.tokens, where), hq = fits_int(q.heads, where), hk = has_k ? fits_int(k.heads, where) : 0, D = fits_int(q.channels, where);
+        device.same(k.t, "k");
+    }
+    void turn(PyObject* positions_o, PyObject* freq_o, PyObject* sections_o, const char* where) {
+        PyObject* const list = PySequence_Tuple(sections_o);
+        if (!list) throw Raised{};
+        const Py_ssize_t n = PyTuple_GET_SIZE(list);
+        int64_t pairs = 0;
+        try {
+            if (n < 1 || n > VQ_MAX_AXES) raise_status(VQ_ERR_SHAPE, where);
+            for (axes = 0; axes < n; ++axes) {
+                sections[axes] = whole(PyTuple_GET_ITEM(list, axes), 0, where);
+                pairs += sections[axes];
+            }
+        } catch (...) {
+            Py_DECREF(list);
+            throw;
+        }
+        Py_DECREF(list);
+        positions = &required(positions_o, at::kInt, "positions");
+        freq = &required(freq_o, at::kFloat, "inv_freq");
+        if (!is_matrix(*positions, axes, q.tokens)) fail(PyExc_ValueError, "positions must have shape [axes, T]");
+        if (!is_vector(*freq, pairs)) fail(PyExc_ValueError, "inv_freq must have shape [sum of sections]");
+        device.same(positions, "positions");
+        device.same(freq, "inv_freq");
+    }
+    void outputs(PyObject* qo_o, PyObject* ko_o) {
+        if (!has_k && ko_o != Py_None) fail(PyExc_ValueError, "k_out without k");
+        qo = HeadsOutput(qo_o, q, "q_out", st);
+        if (has_k) ko = HeadsOutput(ko_o, k, "k_out", st);
+        device.same(&qo.t, "q_out");
+        if (has_k) device.same(&ko.t, "k_out");
+        const Heads qv = qo.view("q_out"), kv = has_k ? ko.view("k_out") : qv;
+        const int64_t s[8] = {q.token_stride, q.head_stride, qv.token_stride, qv.head_stride, k.token_stride, k.head_stride, kv.token_stride, kv.head_stride};
+        memcpy(strides, s, sizeof(s));
+    }
+    void* k_in() const { return has_k ? ptr(k.t) : nullptr; }
+    void* k_out() const { return has_k ? ptr(ko.t) : nullptr; }
+    PyObject* release() {
+        PyObject* const first_out = qo.release();
+        if (has_k) return tuple_of(first_out, ko.release());
+        Py_INCREF(Py_None);
+        return tuple_of(first_out, Py_None);
+    }
+};
+
+PyObject* rotary_axes(PyObject* const* a) {  // q k positions inv_freq sections pairing amplitude q_out k_out stream
+    AxesCall c(a[0], a[1], a[9], "vq_rotary_axes");
+    c.turn(a[2], a[3], a[4], "vq_rotary_axes");
+    const int pairing = whole(a[5], 0, "vq_rotary_axes");
+    const float amplitude = (float)number(a[6]);
+    c.outputs(a[7], a[8]);
+    enqueue("vq_rotary_axes", g_lib.rotary_axes, ptr(c.q.t), ptr(c.qo.t), c.k_in(), c.k_out(), c.code, as<int32_t>(c.positions), as<float>(c.freq),
+            amplitude, pairing, c.axes, (const int32_t*)c.sections, c.T, c.hq, c.hk, c.D, (const int64_t*)c.strides, c.st.handle());
+    return c.release();
+}
+
+// q k q_weight k_weight q_bias k_bias norm eps positions inv_freq sections pairing amplitude q_out k_out stream
+PyObject* norm_rotary(PyObject* const* a) {
+    AxesCall c(a[0], a[1], a[15], "vq_norm_rotary");
+    const at::Tensor* vectors[4];
+    static const char* const names[4] = {"q_weight", "k_weight", "q_bias", "k_bias"};
+    for (int i = 0; i < 4; ++i) {
+        vectors[i] = device_tensor(a[2 + i], at::kFloat, names[i]);
+        if (vectors[i] && !is_vector(*vectors[i], c.q.channels)) {
+            PyErr_Format(PyExc_ValueError, "%s must have shape [head_dim]", names[i]);
+            throw Raised{};
+        }
+        if (vectors[i] && i % 2 == 1 && !c.has_k) {
+            PyErr_Format(PyExc_ValueError, "%s without k", names[i]);
+            throw Raised{};
+        }
+        c.device.same(vectors[i], names[i]);
+    }
+    const int norm = whole(a[6], 0, "vq_norm_rotary");
+    const float eps = (float)number(a[7]);
+    if (a[10] != Py_None)
+        c.turn(a[8], a[9], a[10], "vq_norm_rotary");
+    else if (a[8] != Py_None || a[9] != Py_None)
+        fail(PyExc_ValueError, "positions and inv_freq need sections");
+    const int pairing = whole(a[11], 0, "vq_norm_rotary");
+    const float amplitude = (float)number(a[12]);
+    c.outputs(a[13], a[14]);
+    enqueue("vq_norm_rotary", g_lib.norm_rotary, ptr(c.q.t), ptr(c.qo.t), c.k_in(), c.k_out(), c.code, norm, eps, as<float>(vectors[0]),
+            as<float>(vectors[2]), as<float>(vectors[1]), as<float>(vectors[3]), as<int32_t>(c.positions), as<float>(c.freq), amplitude, pairing, c.axes,
+            (const int32_t*)c.sections, c.T, c.hq, c.hk, c.D, (const int64_t*)c.strides, c.st.handle());
+    return c.release();
+}
+
+// What the forms of attention share: views of q, k and v, the sequences' offsets, scale, output and workspace.
+struct AttentionCall {
+    const at::Tensor& first;
+    const int code;
+    const OnDevice device;
+    const CallStream st;
+    const Heads q, k, v;
+    const at::Tensor &cu_q, &cu_k;
+    int B, Tq, Tk, H, G, D, causal;
+    float scale;
+    HeadsOutput out;
+    at::Tensor workspace;
+    AttentionCall(PyObject* q_o, PyObject* k_o, PyObject* v_o, PyObject* cu_q_o, PyObject* cu_k_o, PyObject* scale_o, PyObject* causal_o,
+                  PyObject* stream, const char* where)
+        : first(some_device_tensor(q_o, "q")), code(type_code(first.scalar_type(), false, "q")), device(first), st(stream), q(first, "q"),
+          k(heads_argument(k_o, first.scalar_type(), "k")), v(heads_argument(v_o, first.scalar_type(), "v")),
+          cu_q(required(cu_q_o, at::kInt, "cu_q")), cu_k(required(cu_k_o, at::kInt, "cu_k")) {
+        if (v.tokens != k.tokens || v.heads != k.heads) fail(PyExc_ValueError, "k and v must have the same tokens and heads");
+        if (k.channels != q.channels || v.channels != q.channels) fail(PyExc_ValueError, "q, k and v must have the same channels");
+        if (cu_q.dim() != 1 || cu_q.size(0) < 1 || !is_vector(cu_k, cu_q.size(0))) fail(PyExc_ValueError, "cu_q and cu_k must have shape [sequences + 1]");
+        scale = scale_o == Py_None ? (float)(1.0 / std::sqrt((double)std::max<int64_t>(q.channels, 1))) : (float)number(scale_o);
+        causal = truth(causal_o);
+        B = fits_int(cu_q.size(0) - 1, where), Tq = fits_int(q.tokens, where), Tk = fits_int(k.tokens, where);
+        H = fits_int(q.heads, where), G = fits_int(k.heads, where), D = fits_int(q.channels, where);
+        device.same(k.t, "k");
+        device.same(v.t, "v");
+        device.same(&cu_q, "cu_q");
+        device.same(&cu_k, "cu_k");
+    }
+    void outputs(PyObject* out_o, PyObject* workspace_o, size_t need) {
+        out = HeadsOutput(out_o, q, "out", st);
+        if (workspace_o != Py_None)
+            workspace = *device_tensor(workspace_o, at::kByte, "workspace");
+        else if (need > 0)
+            workspace = st.empty({(int64_t)need}, at::kByte, first, false);
+        if (workspace.defined()) device.same(&workspace, "workspace");
+        device.same(&out.t, "out");
+    }
+    size_t bytes() const { return workspace.defined() ? (size_t)workspace.numel() : 0; }
+    void* scratch() const { return bytes() ? ptr(workspace) : nullptr; }
+};
+
+// q k v cu_q cu_k left right sinks softmax_scale causal out workspace stream
+PyObject* attention_window(PyObject* const* a) {
+    static const char* const where = "vq_attention_window";
+    AttentionCall c(a[0], a[1], a[2], a[3], a[4], a[8], a[9], a[12], where);
+    const int left = whole(a[5], -1, where), right = whole(a[6], -1, where), sinks = whole(a[7], 0, where);
+    c.outputs(a[10], a[11], g_lib.attention_window_workspace_bytes(c.B, c.Tq, c.Tk, c.H, c.G, c.D, c.causal, left, right, sinks));
+    const Heads o = c.out.view("out");
+    const int64_t strides[8] = {c.q.token_stride, c.q.head_stride, c.k.token_stride, c.k.head_stride,
+                                c.v.token_stride, c.v.head_stride, o.token_stride, o.head_stride};
+    enqueue(where, g_lib.attention_window, ptr(c.q.t), ptr(c.k.t), ptr(c.v.t), ptr(c.out.t), c.code, as<int32_t>(c.cu_q), as<int32_t>(c.cu_k), c.B, c.Tq,
+            c.Tk, c.H, c.G, c.D, (const int64_t*)strides, c.scale, c.causal, left, right, sinks, c.scratch(), c.bytes(), c.st.handle());
+    return c.out.release();
+}
+
+// q prefix_k prefix_v k v cu_q cu_k softmax_scale causal out workspace stream
+PyObject* attention_prefix(PyObject* const* a) {
+    static const char* const where = "vq_attention_prefix";
+    AttentionCall c(a[0], a[3], a[4], a[5], a[6], a[7], a[8], a[11], where);
+    const Heads pk = heads_argument(a[1], c.first.scalar_type(), "prefix_k"), pv = heads_argument(a[2], c.first.scalar_type(), "prefix_v");
+    if (pv.tokens != pk.tokens) fail(PyExc_ValueError, "prefix_k and prefix_v must have the same tokens");
+    if (pk.heads != c.k.heads || pv.heads != c.k.heads || pk.channels != c.k.channels || pv.channels != c.k.channels)
+        fail(PyExc_ValueError, "prefix_k and prefix_v must have the heads and channels of k");
+    const int P = fits_int(pk.tokens, where);
+    c.device.same(pk.t, "prefix_k");
+    c.device.same(pv.t, "prefix_v");
+    c.outputs(a[9], a[10], g_lib.attention_prefix_workspace_bytes(c.B, c.Tq, P, c.Tk, c.H, c.G, c.D));
+    const Heads o = c.out.view("out");
+    const int64_t strides[12] = {c.q.token_stride, c.q.head_stride, pk.token_stride, pk.head_stride, pv.token_stride, pv.head_stride,
+                                 c.k.token_stride, c.k.head_stride, c.v.token_stride, c.v.head_stride, o.token_stride, o.head_stride};
+    enqueue(where, g_lib.attention_prefix, ptr(c.q.t), ptr(pk.t), ptr(pv.t), ptr(c.k.t), ptr(c.v.t), ptr(c.out.t), c.code, as<int32_t>(c.cu_q),
+            as<int32_t>(c.cu_k), c.B, c.Tq, P, c.Tk, c.H, c.G, c.D, (const int64_t*)strides, c.scale, c.causal, c.scratch(), c.bytes(), c.st.handle());
+    return c.out.release();
+}
+
 // ---- module ------------------------------------------------------------------------------------
 
 // bind(vq_error, addresses): the exception class and the entry points' addresses in Entries' order.
@@ -946,6 +1149,10 @@ PyMethodDef g_methods[] = {
     VQ_ENTRY(linear_mx4, 8),
     VQ_ENTRY(rotary, 9),
     VQ_ENTRY(attention, 10),
+    VQ_ENTRY(rotary_axes, 10),
+    VQ_ENTRY(norm_rotary, 16),
+    VQ_ENTRY(attention_window, 13),
+    VQ_ENTRY(attention_prefix, 12),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_vq_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
