@@ -12,9 +12,9 @@ namespace vq {
 // A kernel of one argument.  (An argument costs the host 0.04 us, the <<<>>> stub 0.15 us beyond the 2.1 that a launch
 // takes; small layers are host-bound.)
 template <class Args>
-inline hipError_t enqueue(void (*kernel)(Args), dim3 grid, dim3 block, hipStream_t stream, const Args& a) {
+inline hipError_t enqueue(void (*kernel)(Args), dim3 grid, dim3 block, hipStream_t stream, const Args& a, size_t lds_bytes = 0) {
     void* args[] = {const_cast<Args*>(&a)};
-    const hipError_t e = hipLaunchKernel((const void*)kernel, grid, block, args, 0, stream);
+    const hipError_t e = hipLaunchKernel((const void*)kernel, grid, block, args, lds_bytes, stream);
     if (e != hipSuccess) (void)hipGetLastError();   // (reported here, not once more by the next call)
     return e;
 }
@@ -133,6 +133,8 @@ struct RotaryAxesArgs {
     int pairing, axes, pairs, sections[VQ_MAX_AXES];
     int T, q_heads, k_heads, head_dim;
     int64_t q_token, q_head, qo_token, qo_head, k_token, k_head, ko_token, ko_head;   // strides in elements
+    int has_bias, tokens_each, heads_each, head_blocks, per_head[2];                  // the launch's: of a workgroup,
+    int64_t blocks;                                                                   // and what workgroups take in turn
 };
 hipError_t launch_rotary_axes(RotaryAxesArgs a, int dtype, hipStream_t stream);
 
