@@ -327,9 +327,9 @@ int validate_workspace(const void* workspace, size_t bytes, size_t need) {
 }
 bool window_ok(int causal, int left, int right, int sinks) { return (causal == 0 || causal == 1) && left >= -1 && right >= -1 && sinks >= 0; }
 // Partial sums, maxima and weights of a call whose keys are divided.
+size_t bytes_of_parts(int parts, int Tq, int heads, int head_dim) { return (size_t)parts * (size_t)Tq * (size_t)heads * (size_t)(head_dim + 2) * sizeof(float); }
 size_t workspace_of(const vq::AttentionChoice& choice, int Tq, int heads, int head_dim) {
-    const size_t parts = (size_t)1 << choice.split_shift;
-    return parts == 1 || !choice.fits ? 0 : parts * (size_t)Tq * (size_t)heads * (size_t)(head_dim + 2) * sizeof(float);
+    return choice.split_shift == 0 || !choice.fits ? 0 : bytes_of_parts(1 << choice.split_shift, Tq, heads, head_dim);
 }
 // strides: token and head of q, k, v, out.
 template <class ARGS>
@@ -802,7 +802,8 @@ int vq_attention_window(const void* q, const void* k, const void* v, void* out, 
 
 size_t vq_attention_prefix_workspace_bytes(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim) {
     if (prefix < 0 || Tk < 0 || !attention_sizes_ok(sequences, Tq, (int64_t)prefix + Tk, heads, kv_heads, head_dim) || sequences == 0 || Tq == 0) return 0;
-    return 0;
+    const vq::AttentionPrefixChoice choice = vq::choose_attention_prefix(sequences, Tq, prefix, Tk, heads, kv_heads);
+    return choice.fits ? bytes_of_parts(choice.parts(), Tq, heads, head_dim) : 0;
 }
 
 int vq_attention_prefix(const void* q, const void* prefix_k, const void* prefix_v, const void* k, const void* v, void* out, int dtype,
@@ -813,6 +814,8 @@ int vq_attention_prefix(const void* q, const void* prefix_k, const void* prefix_
         !attention_scale_ok(softmax_scale))
         return VQ_ERR_SHAPE;
     if (sequences == 0 || Tq == 0) return VQ_OK;
+    const vq::AttentionPrefixChoice choice = vq::choose_attention_prefix(sequences, Tq, prefix, Tk, heads, kv_heads);
+    if (!choice.fits) return VQ_ERR_SHAPE;
     if (!strides) return VQ_ERR_NULL;
     int status = validate_views({{q, strides, Tq, heads, View::kQueries}, {prefix_k, strides + 2, prefix, kv_heads, View::kKeys},
                                  {prefix_v, strides + 4, prefix, kv_heads, View::kKeys}, {k, strides + 6, Tk, kv_heads, View::kKeys},
@@ -825,7 +828,10 @@ int vq_attention_prefix(const void* q, const void* prefix_k, const void* prefix_
     set_attention(a, q, k, v, out, cu_q, cu_k, sequences, Tq, Tk, heads, kv_heads, head_dim, own, softmax_scale, causal);
     a.prefix_k = prefix_k, a.prefix_v = prefix_v, a.prefix = prefix;
     a.pk_token = strides[2], a.pk_head = strides[3], a.pv_token = strides[4], a.pv_head = strides[5];
-    return launch_status(vq::launch_attention_prefix(a, dtype, (hipStream_t)hip_stream));
+    a.split_shift = choice.split_shift;
+    a.part_o = (float*)workspace;
+    a.part_ml = a.part_o ? a.part_o + (size_t)choice.parts() * Tq * heads * head_dim : nullptr;
+    return launch_status(vq::launch_attention_prefix(a, choice, dtype, (hipStream_t)hip_stream));
 }
 
 const char* vq_status_string(int status) {

@@ -18,6 +18,8 @@
 //
 // Query heads that share a head of K and V are rows of one tile: row r of a sequence is token r / group, head r % group.
 #pragma once
+#include <type_traits>
+
 #include "vq_gemm_common.h"
 #include "vq_internal.h"
 #include "vq_types.h"
@@ -28,6 +30,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char* lds_bytes;
+constexpr float kInf = __builtin_inff();
 
 // ---- sequences -----------------------------------------------------------------------------------------------
 
@@ -44,6 +47,9 @@ __device__ __forceinline__ Span span_of(const AttentionArgs& a, int b) {
     return s;
 }
 
+// (all query rows are one sequence's, to the keys that every sequence shares)
+__device__ __forceinline__ Span span_of(const AttentionSharedArgs& a, int) { return {0, a.Tq, 0, a.Tk}; }
+
 __device__ __forceinline__ int token_of(const AttentionArgs& a, int row) {
     return a.group_shift >= 0 ? row >> a.group_shift : (int)((unsigned)row / (unsigned)a.group);
 }
@@ -51,6 +57,10 @@ __device__ __forceinline__ int token_of(const AttentionArgs& a, int row) {
 __device__ __forceinline__ int keys_seen(const AttentionArgs& a, const Span& s, int token) {
     return a.causal ? min(s.m, max(0, s.m - s.n + token + 1)) : s.m;
 }
+// Whether a row's outputs are parts, joined later.
+__device__ __forceinline__ bool writes_parts(const AttentionArgs& a) { return a.split_shift != 0; }
+__device__ __forceinline__ bool writes_parts(const AttentionSharedArgs&) { return true; }
+__device__ __forceinline__ bool writes_parts(const AttentionOwnArgs&) { return true; }
 // Tiles of keys of a workgroup among those that divide `tiles` (less than 2^26 of them; at most 2^6 workgroups).
 __device__ __forceinline__ int split_begin(const AttentionArgs& a, int tiles, int split) {
     return (int)((unsigned)tiles * (unsigned)split >> a.split_shift);
@@ -83,6 +93,129 @@ inline unsigned attention_grid(AttentionArgs& a, long tiles) {
     const long items = a.heads_together ? ((long)a.items + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds : a.items;
     return (unsigned)(items * a.kv_heads);
 }
+
+// ---- which keys there are ------------------------------------------------------------------------------------
+// The keys that a block of a sequence's query rows works on, in tiles of N, for the arguments ARGS; tokens ascend along the block's rows.
+
+// All of the sequence's, or, causal, up to a token's own place.
+template <class ARGS, class T, int N>
+struct Keys {
+    static constexpr bool kFirstSeen = true;       // a row that sees any key sees the first of its first tile
+    static constexpr bool kTwoTensors = false;
+    struct Row {                                   // what one row sees
+        int visible;
+        __device__ __forceinline__ Row(const ARGS& a, const Span& s, int token) : visible(keys_seen(a, s, token)) {}
+    };
+    struct Rows {                                  // what all rows from one token to another see
+        int least;
+        __device__ __forceinline__ Rows(const ARGS& a, const Span& s, int first, int) : least(__builtin_amdgcn_readfirstlane(keys_seen(a, s, first))) {}
+    };
+    const T *k, *v;
+    int m, tiles;
+    __device__ __forceinline__ Keys(const ARGS& a, const Span& s, int kv, int, int last)
+        : k((const T*)a.k + s.k0 * a.k_token + kv * a.k_head), v((const T*)a.v + s.k0 * a.v_token + kv * a.v_head), m(s.m),
+          tiles((__builtin_amdgcn_readfirstlane(keys_seen(a, s, last)) + N - 1) / N) {}
+    __device__ __forceinline__ int left(int t) const { return m - t * N; }         // keys from the tile's first on
+    __device__ __forceinline__ const T* k_of(const ARGS& a, int t) const { return k + (long)t * N * a.k_token; }
+    __device__ __forceinline__ const T* v_of(const ARGS& a, int t) const { return v + (long)t * N * a.v_token; }
+    __device__ __forceinline__ bool whole(const Rows& r, int t) const { return t * N + N <= r.least; }
+    __device__ __forceinline__ int key_of_tile(int t) const { return t * N; }
+    __device__ __forceinline__ Row within(const Row& r, int) const { return r; }                       // what a row sees of a tile
+    __device__ __forceinline__ bool sees(const Row& r, int key) const { return key < r.visible; }      // (r: within the key's tile)
+};
+
+// Those of a window and the sequence's first: the first ones' tiles, then tiles from the first key on that any row's window has.  What no row of
+// the block sees is not loaded.
+template <class T, int N>
+struct Keys<AttentionWindowArgs, T, N> {
+    static constexpr bool kFirstSeen = false;
+    static constexpr bool kTwoTensors = false;
+    struct Row {
+        int lo, size, sinks;                       // the window's first key, how many it has, first keys
+        __device__ __forceinline__ Row(const AttentionWindowArgs& a, const Span& s, int token) {
+            const int ahead = s.n - token, p = s.m - ahead;                        // p = token + m - n; ahead >= 1
+            const int hi = a.causal ? max(p + 1, 0) : a.right < 0 || a.right >= ahead - 1 ? s.m : max(p + a.right + 1, 0);
+            lo = max(max(p, 0) - a.left, 0);
+            size = max(hi - lo, 0);
+            sinks = min(a.sinks, a.causal ? hi : s.m);
+        }
+    };
+    struct Rows {
+        int lo, hi, sinks;
+        __device__ __forceinline__ Rows(const AttentionWindowArgs& a, const Span& s, int first, int last) {
+            const Row f(a, s, first), l(a, s, last);
+            lo = __builtin_amdgcn_readfirstlane(l.lo);
+            hi = __builtin_amdgcn_readfirstlane(f.lo + f.size);
+            sinks = __builtin_amdgcn_readfirstlane(f.sinks);
+        }
+    };
+    const T *k, *v;
+    int sinks, first_tiles, start, end, tiles;
+    __device__ __forceinline__ Keys(const AttentionWindowArgs& a, const Span& s, int kv, int first, int last)
+        : k((const T*)a.k + s.k0 * a.k_token + kv * a.k_head), v((const T*)a.v + s.k0 * a.v_token + kv * a.v_head) {
+        const Row f(a, s, first), l(a, s, last);
+        sinks = __builtin_amdgcn_readfirstlane(l.sinks);
+        start = __builtin_amdgcn_readfirstlane(f.lo);
+        end = __builtin_amdgcn_readfirstlane(l.lo + l.size);
+        if (start <= sinks) {                      // (one stretch of keys)
+            end = max(end, sinks);
+            start = sinks = 0;
+        }
+        first_tiles = (sinks + N - 1) / N;
+        tiles = first_tiles + (max(end - start, 0) + N - 1) / N;
+    }
+    __device__ __forceinline__ int key_of_tile(int t) const { return t < first_tiles ? t * N : start + (t - first_tiles) * N; }
+    __device__ __forceinline__ int left(int t) const { return (t < first_tiles ? sinks : end) - key_of_tile(t); }
+    __device__ __forceinline__ const T* k_of(const AttentionWindowArgs& a, int t) const { return k + key_of_tile(t) * a.k_token; }
+    __device__ __forceinline__ const T* v_of(const AttentionWindowArgs& a, int t) const { return v + key_of_tile(t) * a.v_token; }
+    __device__ __forceinline__ bool whole(const Rows& r, int t) const {
+        const int key = key_of_tile(t);
+        return (key >= r.lo && key + N <= r.hi) || key + N <= r.sinks;
+    }
+    // (the first ones' last tile has no keys behind them, whatever the window)
+    __device__ __forceinline__ Row within(Row r, int t) const {
+        if (t < first_tiles) r.size = 0;
+        return r;
+    }
+    __device__ __forceinline__ bool sees(const Row& r, int key) const { return (unsigned)(key - r.lo) < (unsigned)r.size || key < r.sinks; }
+};
+
+// Keys that all sequences share, then the sequence's own as in the first.
+template <class T, int N>
+struct Keys<AttentionPrefixArgs, T, N> {
+    static constexpr bool kFirstSeen = true;
+    static constexpr bool kTwoTensors = true;
+    struct Row {
+        int visible;                               // of its own
+        __device__ __forceinline__ Row(const AttentionPrefixArgs& a, const Span& s, int token) : visible(keys_seen(a, s, token)) {}
+    };
+    struct Rows {
+        int least;
+        __device__ __forceinline__ Rows(const AttentionPrefixArgs& a, const Span& s, int first, int) : least(__builtin_amdgcn_readfirstlane(keys_seen(a, s, first))) {}
+    };
+    const T *pk, *pv, *k, *v;
+    int prefix, m, first_tiles, tiles;
+    __device__ __forceinline__ Keys(const AttentionPrefixArgs& a, const Span& s, int kv, int, int last)
+        : pk((const T*)a.prefix_k + kv * a.pk_head), pv((const T*)a.prefix_v + kv * a.pv_head), k((const T*)a.k + s.k0 * a.k_token + kv * a.k_head),
+          v((const T*)a.v + s.k0 * a.v_token + kv * a.v_head), prefix(a.prefix), m(s.m), first_tiles((a.prefix + N - 1) / N),
+          tiles(first_tiles + (__builtin_amdgcn_readfirstlane(keys_seen(a, s, last)) + N - 1) / N) {}
+    __device__ __forceinline__ int left(int t) const { return t < first_tiles ? prefix - t * N : m - (t - first_tiles) * N; }
+    __device__ __forceinline__ const T* k_of(const AttentionPrefixArgs& a, int t) const {
+        return t < first_tiles ? pk + (long)t * N * a.pk_token : k + (long)(t - first_tiles) * N * a.k_token;
+    }
+    __device__ __forceinline__ const T* v_of(const AttentionPrefixArgs& a, int t) const {
+        return t < first_tiles ? pv + (long)t * N * a.pv_token : v + (long)(t - first_tiles) * N * a.v_token;
+    }
+    __device__ __forceinline__ bool whole(const Rows& r, int t) const {
+        return t < first_tiles ? t * N + N <= prefix : (t - first_tiles) * N + N <= r.least;
+    }
+    __device__ __forceinline__ int key_of_tile(int t) const { return (t < first_tiles ? t : t - first_tiles) * N; }
+    __device__ __forceinline__ Row within(Row r, int t) const {
+        if (t < first_tiles) r.visible = prefix;
+        return r;
+    }
+    __device__ __forceinline__ bool sees(const Row& r, int key) const { return key < r.visible; }
+};
 
 // ---- tiles of K and V in LDS ---------------------------------------------------------------------------------
 // [key][CHUNKS of 16 bytes], the chunk of a key at chunk ^ swizzle(key), so that what the LDS serves at once lies in different banks:
@@ -186,10 +319,10 @@ __device__ __forceinline__ constexpr int key_of(int r) { return (r & 3) + 8 * (r
 
 // A wavefront's 32 rows of outputs, whose lanes' sums l and outputs o (relative to ref) are complete: normalised to `out`, or as they are
 // to the parts.  `row`: token (of all) and head of the lane's row.
-template <class TYPE, int BLOCKS>
-__device__ __forceinline__ void write_rows(const AttentionArgs& a, const v16f* o, float ref, float l, int token, int head, int split, bool real, int half) {
+template <class TYPE, int BLOCKS, class ARGS>
+__device__ __forceinline__ void write_rows(const ARGS& a, const v16f* o, float ref, float l, int token, int head, int split, bool real, int half) {
     typedef typename TYPE::T T;
-    if (a.split_shift == 0) {
+    if (!writes_parts(a)) {
         const float inv = l > 0 ? 1.0f / l : 0.0f;
         T* const y = (T*)a.out + token * a.o_token + head * a.o_head;
 #pragma unroll

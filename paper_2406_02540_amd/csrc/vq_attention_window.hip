@@ -1,36 +1,40 @@
-// Attention in a sliding window with first keys that stay visible.
-#include "vq_attention_simple.h"
+// Attention in a sliding window with first keys that stay visible: the kernels of vq_attention on the tiles of keys that a block of query rows sees.
+#include "vq_attention_rows_kernel.h"
+#include "vq_attention_tiles_kernel.h"
 
 namespace vq {
-namespace {
 
-struct WindowKeys {
-    const AttentionWindowArgs& a;
-    const Span& s;
-    int kv, p, count;
-    __device__ WindowKeys(const AttentionWindowArgs& a, const Span& s, int token, int kv) : a(a), s(s), kv(kv), p(token + s.m - s.n), count(s.m) {}
-    __device__ bool seen(int key) const {
-        const long d = (long)key - p;
-        return ((d >= -a.left && (a.right < 0 || d <= a.right)) || key < a.sinks) && !(a.causal && d > 0);
-    }
-    template <class T>
-    __device__ const T* k(int key) const { return (const T*)a.k + (s.k0 + key) * a.k_token + kv * a.k_head; }
-    template <class T>
-    __device__ const T* v(int key) const { return (const T*)a.v + (s.k0 + key) * a.v_token + kv * a.v_head; }
-};
-
-template <class TYPE>
-__global__ __launch_bounds__(256) void attention_window(AttentionWindowArgs a) {
-    attention_simple<TYPE, AttentionWindowArgs, WindowKeys>(a);
+AttentionChoice choose_attention_window(int sequences, int Tq, int Tk, int heads, int kv_heads, int causal, int left, int right, int sinks) {
+    const int group = heads / kv_heads;
+    // Keys that a block of the average sequence's rows works on.
+    const long all = (long)Tk / sequences, queries = ((long)Tq + sequences - 1) / sequences;
+    const bool rows = (long)Tq * group <= 32l * sequences;
+    const long tokens = rows ? (queries < 32 / group + 1 ? queries : 32 / group + 1) : queries < kTileRows / group + 1 ? queries : kTileRows / group + 1;
+    long keys = sinks + tokens;
+    keys = left < 0 ? all : keys + left;
+    if (!causal) keys = right < 0 ? all : keys + right;
+    if (keys > all) keys = all;
+    const long tiles = rows ? (long)sequences : attention_items(sequences, Tq, group), items = tiles * kv_heads;
+    int shift = 0;
+    while (shift < 6 && (items << shift) < (rows ? 2048 : 512) && keys >> (shift + 1) >= 256) ++shift;
+    const bool alone = rows && shift == 0 && keys <= 64 && (long)sequences * kv_heads >= 2048;
+    const long most = ((tiles << shift) + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds * kv_heads;
+    return {!rows ? kAttentionTiles : alone ? kAttentionRowsAlone : kAttentionRows, shift, most * (alone ? 64 : 256) < 1l << 32};
 }
 
-}  // namespace
-
-AttentionChoice choose_attention_window(int, int, int, int, int, int, int, int, int) { return {kAttentionRows, 0, true}; }
-
-hipError_t launch_attention_window(const AttentionWindowArgs& a, AttentionKernel, int dtype, hipStream_t stream) {
-    const long blocks = ((long)a.Tq * a.heads + 3) / 4;
-    return enqueue(dtype == VQ_F16 ? attention_window<F16> : attention_window<BF16>, dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)), dim3(256), stream, a);
+hipError_t launch_attention_window(const AttentionWindowArgs& a, AttentionKernel kernel, int dtype, hipStream_t stream) {
+    const bool f16 = dtype == VQ_F16;
+    if (kernel == kAttentionRowsAlone) return f16 ? launch_rows<F16, 1, 1>(a, stream) : launch_rows<BF16, 1, 1>(a, stream);
+    const hipError_t e = kernel == kAttentionTiles ? (f16 ? launch_tiles<F16>(a, stream) : launch_tiles<BF16>(a, stream))
+                         : f16                     ? launch_rows<F16, 4, 2>(a, stream)
+                                                   : launch_rows<BF16, 4, 2>(a, stream);
+    return e != hipSuccess || a.split_shift == 0 ? e : launch_join<AttentionArgs>(a, dtype, stream);
 }
 
 }  // namespace vq
+
+extern "C" void vq_internal_attention_window_choice(int sequences, int Tq, int Tk, int heads, int kv_heads, int causal, int left, int right, int sinks, int choice[2]) {
+    const vq::AttentionChoice c = vq::choose_attention_window(sequences, Tq, Tk, heads, kv_heads, causal, left, right, sinks);
+    choice[0] = c.kernel;
+    choice[1] = c.split_shift;
+}
