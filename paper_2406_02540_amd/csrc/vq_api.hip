@@ -802,7 +802,7 @@ int vq_attention_window(const void* q, const void* k, const void* v, void* out, 
 
 size_t vq_attention_prefix_workspace_bytes(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim) {
     if (prefix < 0 || Tk < 0 || !attention_sizes_ok(sequences, Tq, (int64_t)prefix + Tk, heads, kv_heads, head_dim) || sequences == 0 || Tq == 0) return 0;
-    const vq::AttentionPrefixChoice choice = vq::choose_attention_prefix(sequences, Tq, prefix, Tk, heads, kv_heads);
+    const vq::AttentionPrefixChoice choice = vq::choose_attention_prefix(sequences, Tq, prefix, Tk, heads, kv_heads, head_dim);
     return choice.fits ? bytes_of_parts(choice.parts(), Tq, heads, head_dim) : 0;
 }
 
@@ -814,7 +814,7 @@ int vq_attention_prefix(const void* q, const void* prefix_k, const void* prefix_
         !attention_scale_ok(softmax_scale))
         return VQ_ERR_SHAPE;
     if (sequences == 0 || Tq == 0) return VQ_OK;
-    const vq::AttentionPrefixChoice choice = vq::choose_attention_prefix(sequences, Tq, prefix, Tk, heads, kv_heads);
+    const vq::AttentionPrefixChoice choice = vq::choose_attention_prefix(sequences, Tq, prefix, Tk, heads, kv_heads, head_dim);
     if (!choice.fits) return VQ_ERR_SHAPE;
     if (!strides) return VQ_ERR_NULL;
     int status = validate_views({{q, strides, Tq, heads, View::kQueries}, {prefix_k, strides + 2, prefix, kv_heads, View::kKeys},

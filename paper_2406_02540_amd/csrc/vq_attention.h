@@ -73,17 +73,25 @@ __device__ __forceinline__ int split_begin(const AttentionArgs& a, int tiles, in
 // that are not in the caches); 2048 sequences of 16 93.7 and 84; heads of 96 34.9 and 33.9.  With many keys they are better by heads: 32
 // sequences of 1024 223 and 232; so are heads of whole lines: of 128 on 128 keys 43 and 45 (both with inputs in the caches).
 constexpr int kAttentionXcds = 8;
-__device__ __forceinline__ bool place_of(const AttentionArgs& a, int& kv, int& item) {
+__device__ __forceinline__ bool place_of(const AttentionArgs& a, unsigned block, int& kv, int& item) {
     if (a.heads_together) {
-        const unsigned j = blockIdx.x / kAttentionXcds, group = j / (unsigned)a.kv_heads;
+        const unsigned j = block / kAttentionXcds, group = j / (unsigned)a.kv_heads;
         kv = (int)(j - group * (unsigned)a.kv_heads);
-        item = (int)(group * kAttentionXcds + blockIdx.x % kAttentionXcds);
+        item = (int)(group * kAttentionXcds + block % kAttentionXcds);
     } else {
-        const unsigned j = blockIdx.x / (unsigned)a.kv_heads;
-        kv = (int)(blockIdx.x - j * (unsigned)a.kv_heads);
+        const unsigned j = block / (unsigned)a.kv_heads;
+        kv = (int)(block - j * (unsigned)a.kv_heads);
         item = (int)j;
     }
     return item < a.items;
+}
+// (one sequence's tiles of rows: those that read the same keys, a part of a head's, follow each other on one XCD)
+__device__ __forceinline__ bool place_of(const AttentionSharedArgs& a, unsigned block, int& kv, int& item) {
+    const unsigned j = block / kAttentionXcds, group = j / (unsigned)a.tiles;
+    const unsigned unit = group * kAttentionXcds + block % kAttentionXcds, split = unit / (unsigned)a.kv_heads;
+    kv = (int)(unit - split * (unsigned)a.kv_heads);
+    item = (int)(((j - group * (unsigned)a.tiles) << a.split_shift) + split);
+    return split >> a.split_shift == 0;
 }
 // The workgroups that place_of() has in mind (choose_attention() has seen that a launch takes them).
 inline unsigned attention_grid(AttentionArgs& a, long tiles) {
@@ -92,6 +100,9 @@ inline unsigned attention_grid(AttentionArgs& a, long tiles) {
     a.heads_together = a.Tk / a.sequences <= 512 && a.head_dim % 64 != 0;
     const long items = a.heads_together ? ((long)a.items + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds : a.items;
     return (unsigned)(items * a.kv_heads);
+}
+inline long shared_blocks(long tiles, int split_shift, int kv_heads) {
+    return (((long)kv_heads << split_shift) + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds * tiles;
 }
 
 // ---- which keys there are ------------------------------------------------------------------------------------

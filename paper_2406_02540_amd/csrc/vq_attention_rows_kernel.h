@@ -33,32 +33,38 @@ __device__ __forceinline__ void write_eight_of_row(const ARGS& a, int token, int
 // and V.  16 sequences of one token over up to 32768 keys, 32 heads on 8 of 128, 170 us, 4.7 TB/s of 791 MB (a copy moves 5.2); 64 over
 // 4096 215 us, 5.0 TB/s; one over 32768 39 us, 3.4 TB/s.  CHUNKS: 16-byte chunks of a key in LDS (8, 12, 16); STEPS: of 16 channels;
 // STAGES: tiles of a wavefront in LDS.
+template <int CHUNKS, int WAVES, int STAGES>
+constexpr int kRowsBytes = [] {       // of LDS: the stages, or where the wavefronts' sums meet
+    constexpr int stages = WAVES * STAGES * 2 * kRowKeys * CHUNKS * 16, sums = WAVES == 1 ? 0 : WAVES * kRows * (8 * CHUNKS + 4 + 2) * 4;
+    return stages > sums ? stages : sums;
+}();
+
+// Workgroup `block` of a launch's.
 template <class TYPE, int CHUNKS, int STEPS, int WAVES, int STAGES, class ARGS>
-__global__ __launch_bounds__(64 * WAVES) void attention_rows(ARGS a) {
+__device__ __forceinline__ void rows_of(const ARGS& a, unsigned block, char* lds) {
     constexpr int BLOCKS = CHUNKS / 4;                 // of 32 channels
     constexpr int kTile = kRowKeys * CHUNKS * 16;         // bytes
     constexpr int kStage = 2 * kTile;                  // K, V
     constexpr int kPitch = 32 * BLOCKS + 4;            // floats of a row where the wavefronts' sums meet
     constexpr int kLoads = 2 * kRowKeys * CHUNKS / 64;    // of a stage, per lane
-    constexpr int kBytes = WAVES * STAGES * kStage;
-    static_assert(WAVES == 1 || WAVES * kRows * (kPitch + 2) * 4 <= kBytes, "the sums fit where the stages were");
-    __shared__ __align__(16) char lds[kBytes];
     typedef typename TYPE::T T;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int half = lane >> 5;
     int kv, item;
-    if (!place_of(a, kv, item)) return;
+    if (!place_of(a, block, kv, item)) return;
     const int split = item & ((1 << a.split_shift) - 1), b = item >> a.split_shift;
     const Span s = span_of(a, b);
     const int rows = s.n * a.group;
     const int head_bytes = 2 * a.head_dim;
-    lds_bytes const own = (lds_bytes)lds + wave * STAGES * kStage;
-    const unsigned base = (unsigned)(uintptr_t)own;
-    const TileLoader<CHUNKS, kRowKeys, 64, false> k_load((int)(2 * a.k_token), head_bytes, lane);
-    const TileLoader<CHUNKS, kRowKeys, 64, true> v_load((int)(2 * a.v_token), head_bytes, lane);
-    const KeyReader<CHUNKS, STEPS> k_read(own, lane);
-    const ValueReader<CHUNKS> v_read(own, lane);
+    lds_bytes const mine_in_lds = (lds_bytes)lds + wave * STAGES * kStage;
+    const unsigned base = (unsigned)(uintptr_t)mine_in_lds;
+    typedef TileLoader<CHUNKS, kRowKeys, 64, false> LoaderK;
+    typedef TileLoader<CHUNKS, kRowKeys, 64, true> LoaderV;
+    LoaderK k_load((int)(2 * a.k_token), head_bytes, lane);
+    LoaderV v_load((int)(2 * a.v_token), head_bytes, lane);
+    const KeyReader<CHUNKS, STEPS> k_read(mine_in_lds, lane);
+    const ValueReader<CHUNKS> v_read(mine_in_lds, lane);
 
     for (int row0 = 0; row0 < rows; row0 += kRows) {
         const int r = min(row0 + (lane & 31), rows - 1);
@@ -70,7 +76,20 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows(ARGS a) {
         const typename KeysOf::Row sight(a, s, token);
         const int t0 = split_begin(a, keys.tiles, split), t1 = split_begin(a, keys.tiles, split + 1);
 
+        bool own = true;            // whether the loaders are those of the sequence's own keys
+        if constexpr (KeysOf::kTwoTensors)
+            if (t0 + wave < keys.first_tiles) {
+                own = false;
+                k_load = LoaderK((int)(2 * a.pk_token), head_bytes, lane);
+                v_load = LoaderV((int)(2 * a.pv_token), head_bytes, lane);
+            }
         auto ask = [&](int t, int to) {
+            if constexpr (KeysOf::kTwoTensors)
+                if (!own && t >= keys.first_tiles) {
+                    own = true;
+                    k_load = LoaderK((int)(2 * a.k_token), head_bytes, lane);
+                    v_load = LoaderV((int)(2 * a.v_token), head_bytes, lane);
+                }
             const int left = keys.left(t);
             const unsigned at = base + to * kStage;
             k_load.ask(keys.k_of(a, t), at, left, lane);
@@ -183,6 +202,12 @@ __global__ __launch_bounds__(64 * WAVES) void attention_rows(ARGS a) {
         }
         __syncthreads();      // the next tile's loads go where the sums were
     }
+}
+
+template <class TYPE, int CHUNKS, int STEPS, int WAVES, int STAGES, class ARGS>
+__global__ __launch_bounds__(64 * WAVES) void attention_rows(ARGS a) {
+    __shared__ __align__(16) char lds[kRowsBytes<CHUNKS, WAVES, STAGES>];
+    rows_of<TYPE, CHUNKS, STEPS, WAVES, STAGES>(a, blockIdx.x, lds);
 }
 
 // Joins the parts of the rows whose keys were divided among workgroups: a wavefront a row, a lane first the weight of one of at most 64

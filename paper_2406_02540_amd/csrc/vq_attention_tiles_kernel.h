@@ -32,17 +32,20 @@ __device__ __forceinline__ int find_sequence(const AttentionSharedArgs&, int ite
     return 0;
 }
 
+template <int CHUNKS>
+constexpr int kTilesBytes = 4 * kTileKeys * CHUNKS * 16;      // of LDS: two tiles of K, two of V
+
+// Workgroup `block` of a launch's.
 template <class TYPE, int CHUNKS, int STEPS, class ARGS>
-__global__ __launch_bounds__(64 * kTileWaves, CHUNKS == 16 ? 2 : 3) void attention_tiles(ARGS a) {
+__device__ __forceinline__ void tiles_of(const ARGS& a, unsigned block, char* lds) {
     constexpr int BLOCKS = CHUNKS / 4;
     constexpr int kTile = kTileKeys * CHUNKS * 16;
     constexpr bool kSumColumn = STEPS == 5;             // heads of 72 and 80 channels leave a part of their last block free
-    __shared__ __align__(16) char lds[4 * kTile];       // two tiles of K, two of V
     typedef typename TYPE::T T;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     int kv, item;
-    if (!place_of(a, kv, item)) return;
+    if (!place_of(a, block, kv, item)) return;
     const int split = item & ((1 << a.split_shift) - 1);
     int tile;
     // (the last tiles of a sequence see the most keys: they go first)
@@ -237,6 +240,12 @@ __global__ __launch_bounds__(64 * kTileWaves, CHUNKS == 16 ? 2 : 3) void attenti
     const int last_lane = opaque(lane), row = min(row0 + 32 * wave + (last_lane & 31), rows - 1), its_token = token_of(a, row);
     write_rows<TYPE, BLOCKS>(a, o, ref, l, s.q0 + its_token, kv * a.group + row - its_token * a.group, split,
                              row0 + 32 * wave + (last_lane & 31) < rows, last_lane >> 5);
+}
+
+template <class TYPE, int CHUNKS, int STEPS, class ARGS>
+__global__ __launch_bounds__(64 * kTileWaves, CHUNKS == 16 ? 2 : 3) void attention_tiles(ARGS a) {
+    __shared__ __align__(16) char lds[kTilesBytes<CHUNKS>];
+    tiles_of<TYPE, CHUNKS, STEPS>(a, blockIdx.x, lds);
 }
 
 template <class TYPE, class ARGS>

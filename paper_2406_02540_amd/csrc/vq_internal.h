@@ -185,15 +185,16 @@ struct AttentionPrefixArgs : AttentionArgs {
     int prefix, parts;        // (parts: for the join)
     int64_t pk_token, pk_head, pv_token, pv_head;
 };
-// In one pass by tiles, or, few rows a sequence, in parts: all rows with the shared keys, by tiles or by rows, and each sequence's with its own.
+// In one pass, or in parts: all rows with the shared keys and each sequence's (by rows) with its own.
 struct AttentionPrefixChoice {
-    bool one_pass, shared_by_rows;
+    bool in_parts;
+    AttentionKernel pass;     // of the one pass, or of the rows with the shared keys
     int split_shift;          // of the one pass, or of the sequences' own keys
     int shared_shift;         // 2^shared_shift parts of the shared keys
     bool fits;
-    int parts() const { return one_pass ? (split_shift ? 1 << split_shift : 0) : (1 << split_shift) + (1 << shared_shift); }
+    int parts() const { return in_parts ? (1 << split_shift) + (1 << shared_shift) : split_shift ? 1 << split_shift : 0; }
 };
-AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads);
+AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim);
 // part_o, part_ml: parts() of them.
 hipError_t launch_attention_prefix(const AttentionPrefixArgs& a, const AttentionPrefixChoice& choice, int dtype, hipStream_t stream);
 // The passes of the parts: AttentionArgs of the shared keys (as keys of one sequence), and of the sequences with their own.
@@ -208,5 +209,5 @@ extern "C" void vq_internal_gemm_choice(int w_bits, int M, int N, int K, int num
 extern "C" void vq_internal_mx4_choice(int M, int N, int K, int num_cus, int choice[3]);
 extern "C" void vq_internal_attention_choice(int sequences, int Tq, int Tk, int heads, int kv_heads, int choice[2]);
 extern "C" void vq_internal_attention_window_choice(int sequences, int Tq, int Tk, int heads, int kv_heads, int causal, int left, int right, int sinks, int choice[2]);
-extern "C" void vq_internal_attention_prefix_choice(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int choice[4]);
+extern "C" void vq_internal_attention_prefix_choice(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim, int choice[4]);
 extern "C" int vq_internal_gemm_out(int N, const void* y, const void* acc_out);
