@@ -25,7 +25,7 @@ AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix,
     while (c.split_shift < 5 && (own_items << c.split_shift) < 512 && own >> (c.split_shift + 1) >= 256) ++c.split_shift;
     c.pass = rows <= 32 ? kAttentionRows : kAttentionTiles;
     const long tiles = c.pass == kAttentionRows ? 1 : (rows + kTileRows - 1) / kTileRows;
-    while (c.shared_shift < 5 && (tiles * kv_heads << c.shared_shift) < 256 && (long)prefix >> (c.shared_shift + 1) >= 256) ++c.shared_shift;
+    while (c.shared_shift < 5 && (tiles * kv_heads << c.shared_shift) < (own_items >= 256 ? 128 : 384) && (long)prefix >> (c.shared_shift + 1) >= 256) ++c.shared_shift;
     c.fits = (groups(sequences, c.split_shift) + shared_blocks(tiles, c.shared_shift, kv_heads)) * 256 < 1l << 32;
     return c;
 }
