@@ -85,6 +85,19 @@ __device__ __forceinline__ bool place_of(const AttentionArgs& a, unsigned block,
     }
     return item < a.items;
 }
+// With a window and heads of no whole lines, runs of items go to one XCD with eight neighbouring heads, whose rows share memory lines of all
+// tensors; the items of a run, neighbouring blocks of rows, share most of their keys too.  2 x 16384 tokens, 16 heads of 72, windows of 2049: 486 us by
+// heads, 472 in runs of one, 457 of eight; of 257: 139, 127 and 125; of 1024, causal: 285, 268, 260.  Heads of 64 are better by heads, 364 and 381.
+constexpr int kHeadsOfRun = 8;
+__device__ __forceinline__ bool place_of(const AttentionWindowArgs& a, unsigned block, int& kv, int& item) {
+    if (a.run == 0) return place_of(static_cast<const AttentionArgs&>(a), block, kv, item);
+    const unsigned x = block % kAttentionXcds, j = block / kAttentionXcds, heads = a.kv_heads, run = a.run;
+    const unsigned which = j / (run * heads), in_run = j - which * (run * heads), group = in_run / (run * kHeadsOfRun);
+    const unsigned together = min(heads - group * kHeadsOfRun, (unsigned)kHeadsOfRun), m = in_run - group * (run * kHeadsOfRun), i = m / together;
+    kv = (int)(group * kHeadsOfRun + m - i * together);
+    item = (int)((which * kAttentionXcds + x) * run + i);
+    return item < a.items;
+}
 // (one sequence's tiles of rows: those that read the same keys, a part of a head's, follow each other on one XCD)
 __device__ __forceinline__ bool place_of(const AttentionSharedArgs& a, unsigned block, int& kv, int& item) {
     const unsigned j = block / kAttentionXcds, group = j / (unsigned)a.tiles;
@@ -93,14 +106,26 @@ __device__ __forceinline__ bool place_of(const AttentionSharedArgs& a, unsigned 
     item = (int)(((j - group * (unsigned)a.tiles) << a.split_shift) + split);
     return split >> a.split_shift == 0;
 }
-// The workgroups that place_of() has in mind (choose_attention() has seen that a launch takes them).
-inline unsigned attention_grid(AttentionArgs& a, long tiles) {
+// The workgroups that place_of() has in mind (the choice of the kernel has seen that a launch takes them); keys: of the average sequence.
+inline unsigned attention_grid(AttentionArgs& a, long tiles, long keys) {
     a.tiles = (int)tiles;
     a.items = (int)(tiles << a.split_shift);
-    a.heads_together = a.Tk / a.sequences <= 512 && a.head_dim % 64 != 0;
+    a.heads_together = keys <= 512 && a.head_dim % 64 != 0;
     const long items = a.heads_together ? ((long)a.items + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds : a.items;
     return (unsigned)(items * a.kv_heads);
 }
+inline unsigned attention_grid(AttentionArgs& a, long tiles) { return attention_grid(a, tiles, a.Tk / a.sequences); }
+inline unsigned attention_grid(AttentionPrefixArgs& a, long tiles) { return attention_grid(a, tiles, (long)a.Tk / a.sequences + a.prefix); }
+inline unsigned attention_grid(AttentionWindowArgs& a, long tiles) {
+    const long keys = keys_in_window(a.sequences, a.Tq, a.Tk, a.group, a.causal, a.left, a.right, a.sinks);
+    const unsigned blocks = attention_grid(a, tiles, keys);
+    // (runs of up to eight items, eight of them an XCD at least)
+    a.run = a.head_dim % 64 == 0 || keys > 4096 || a.items < 8 * kAttentionXcds ? 0 : a.items < 64 * kAttentionXcds ? a.items / (8 * kAttentionXcds) : 8;
+    if (a.run == 0) return blocks;
+    const long unit = kAttentionXcds * a.run;
+    return (unsigned)((a.items + unit - 1) / unit * unit * a.kv_heads);
+}
+constexpr int kItemsRounded = 8 * kAttentionXcds;      // a launch's items are rounded up to a divisor of this many
 inline long shared_blocks(long tiles, int split_shift, int kv_heads) {
     return (((long)kv_heads << split_shift) + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds * tiles;
 }

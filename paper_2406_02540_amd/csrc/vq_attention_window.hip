@@ -4,21 +4,24 @@
 
 namespace vq {
 
+long keys_in_window(int sequences, int Tq, int Tk, int group, int causal, int left, int right, int sinks) {
+    const long all = (long)Tk / sequences, queries = ((long)Tq + sequences - 1) / sequences;
+    const long block = ((long)Tq * group <= 32l * sequences ? 32 : kTileRows) / group + 1;       // tokens of a block of rows
+    if (left < 0 || (right < 0 && !causal)) return all;
+    const long keys = (queries < block ? queries : block) + left + (causal ? 0 : right) + sinks;
+    return keys < all ? keys : all;
+}
+
+// As choose_attention(), with the keys that a block of rows works on in the place of the sequence's.
 AttentionChoice choose_attention_window(int sequences, int Tq, int Tk, int heads, int kv_heads, int causal, int left, int right, int sinks) {
     const int group = heads / kv_heads;
-    // Keys that a block of the average sequence's rows works on.
-    const long all = (long)Tk / sequences, queries = ((long)Tq + sequences - 1) / sequences;
+    const long keys = keys_in_window(sequences, Tq, Tk, group, causal, left, right, sinks);
     const bool rows = (long)Tq * group <= 32l * sequences;
-    const long tokens = rows ? (queries < 32 / group + 1 ? queries : 32 / group + 1) : queries < kTileRows / group + 1 ? queries : kTileRows / group + 1;
-    long keys = sinks + tokens;
-    keys = left < 0 ? all : keys + left;
-    if (!causal) keys = right < 0 ? all : keys + right;
-    if (keys > all) keys = all;
     const long tiles = rows ? (long)sequences : attention_items(sequences, Tq, group), items = tiles * kv_heads;
     int shift = 0;
     while (shift < 6 && (items << shift) < (rows ? 2048 : 512) && keys >> (shift + 1) >= 256) ++shift;
     const bool alone = rows && shift == 0 && keys <= 64 && (long)sequences * kv_heads >= 2048;
-    const long most = ((tiles << shift) + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds * kv_heads;
+    const long most = ((tiles << shift) + kItemsRounded) * kv_heads;
     return {!rows ? kAttentionTiles : alone ? kAttentionRowsAlone : kAttentionRows, shift, most * (alone ? 64 : 256) < 1l << 32};
 }
 

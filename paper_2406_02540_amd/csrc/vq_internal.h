@@ -174,7 +174,10 @@ hipError_t launch_attention_tiles(const AttentionArgs& a, int dtype, hipStream_t
 // Attention in a sliding window (vq_attention_window.hip): keys p - left .. p + right (right < 0: no limit) and the first sinks.
 struct AttentionWindowArgs : AttentionArgs {
     int left, right, sinks;
+    int run;                  // the launch's: items that follow each other on an XCD, 0: a head's items go to one
 };
+// Keys that a block of the average sequence's rows works on, at most.
+long keys_in_window(int sequences, int Tq, int Tk, int group, int causal, int left, int right, int sinks);
 AttentionChoice choose_attention_window(int sequences, int Tq, int Tk, int heads, int kv_heads, int causal, int left, int right, int sinks);
 hipError_t launch_attention_window(const AttentionWindowArgs& a, AttentionKernel kernel, int dtype, hipStream_t stream);
 
