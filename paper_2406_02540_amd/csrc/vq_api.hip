@@ -741,7 +741,7 @@ int vq_norm_rotary(const void* q, void* q_out, const void* k, void* k_out, int d
                    const int32_t* sections, int T, int q_heads, int k_heads, int head_dim, const int64_t* strides,
                    void* hip_stream) {
     if (dtype != VQ_F16 && dtype != VQ_BF16) return VQ_ERR_TYPE;
-    if (!rotary_sizes_ok(T, q_heads, k_heads, head_dim) || (norm != VQ_NORM_RMS && norm != VQ_NORM_LAYER) || !(eps > 0.0f) || !std::isfinite(eps) ||
+    if (!rotary_sizes_ok(T, q_heads, k_heads, head_dim) || (norm != VQ_NORM_RMS && norm != VQ_NORM_LAYER) || !(eps >= 1e-30f && eps <= 1e30f) ||
         axes < 0 || (axes > 0 && !std::isfinite(amplitude)))
         return VQ_ERR_SHAPE;
     int pairs = 0;

@@ -14,10 +14,10 @@ namespace vq {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kAtOnce = 4;          // loads of a lane on their way together
+constexpr int kAtOnce = 2;          // rows of a lane that are worked on together
 constexpr int kMaxTokens = 8;       // of a workgroup: their tables are in LDS
-constexpr int kMostTurns = 8;       // of a wavefront, where a workgroup has several tokens
-constexpr int kMaxHeads = 512;      // of a workgroup
+constexpr int kResident = 6 * 256;  // workgroups of a launch at a time, six a CU
+constexpr size_t kLds = 26 << 10;   // bytes of LDS that let them be so many
 constexpr int kStage = 1024;        // bytes of a wavefront's rows, 16 a lane
 
 // Channels of pair `pair`, `first` the pairs of the axes in front of its own, `size` those of its axis.
@@ -93,19 +93,32 @@ __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// The sums over a row's lanes, `pieces` of them from lane - piece on.
-template <int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], int pieces, int piece, int lane) {
-    for (int i = 1; i < pieces; i *= 2) {
-        float o[N];
+// Sums over the lanes of a row, kAtOnce of them: every lane writes its own and reads its row's, four a read, the places behind the last zero.
+// (Through LDS the row's lanes are two ways apart; by exchanges, of which nine lanes take five one behind the other, it took 74 us
+// instead of XX at 32768 tokens, 16 + 16 heads of 72.)
+struct RowSums {
+    float* const mine;
+    const float* const row;
+    const int quads, next;          // floats from one sum's to the next one's
+    __device__ __forceinline__ RowSums(float* at, int rows, int pieces, int row_in, int piece)
+        : mine(at + row_in * (4 * ((pieces + 3) / 4)) + piece), row(at + row_in * (4 * ((pieces + 3) / 4))), quads((pieces + 3) / 4), next(rows * 4 * ((pieces + 3) / 4)) {}
+    __device__ __forceinline__ void operator()(float (&v)[kAtOnce], bool active) const {
+        if (active)
 #pragma unroll
-        for (int n = 0; n < N; ++n) o[n] = __shfl_down(v[n], i);
+            for (int u = 0; u < kAtOnce; ++u) mine[u * next] = v[u];
+        wave_fence();
+        v4f s[kAtOnce];
 #pragma unroll
-        for (int n = 0; n < N; ++n) v[n] += piece + i < pieces ? o[n] : 0.0f;
+        for (int u = 0; u < kAtOnce; ++u) s[u] = active ? *(const v4f*)(row + u * next) : v4f{0, 0, 0, 0};
+        for (int i = 1; i < quads; ++i)
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u)
+                if (active) s[u] += *(const v4f*)(row + u * next + 4 * i);
+        wave_fence();
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) v[u] = (s[u][0] + s[u][1]) + (s[u][2] + s[u][3]);
     }
-#pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = __shfl(v[n], lane - piece);
-}
+};
 
 // What a turn of a wavefront works on: rows of q or of k, all the same for its lanes.
 struct Side {
@@ -118,13 +131,15 @@ struct Side {
 // A lane has eight channels of a row (a head of a token), as many rows a wavefront as fit it: loads and stores are 16 bytes a lane and
 // a token's heads lie next to each other.  Partners are read where the wavefront's rows pass through LDS, GRAIN channels at once: as many as
 // every axis' pairs divide by (0: neighbours, which a lane has itself).  NORM: 0, or 1 + vq_norm.  WIDE: a workgroup's rows are more than 2^31
-// bytes apart.  kAtOnce rows of a lane are worked on together, the next ones' loads on their way meanwhile.
+// bytes apart.  kAtOnce rows of a lane are worked on together, the next ones' loads on their way meanwhile; six workgroups a CU cover each
+// other's waits.  32768 tokens, 16 + 16 heads of 72, f16: turned 50 us (6.0 TB/s), normed and turned 55 us (5.5), with mean, variance and biases 65; with four rows
+// at once, four workgroups a CU, 58, 67 and 82; one row, seven a CU, 52, 59 and 70 (inputs that are not in the caches).
 template <class TYPE, int GRAIN, int NORM, bool WIDE>
-__global__ __launch_bounds__(64 * kWaves) void rotary_axes(RotaryAxesArgs a) {
+__global__ __launch_bounds__(64 * kWaves, WIDE || GRAIN == 1 ? 5 : 6) void rotary_axes(RotaryAxesArgs a) {
     typedef typename TYPE::T T;
     typedef typename std::conditional<WIDE, int64_t, unsigned>::type Offset;
     extern __shared__ __align__(16) char lds[];
-    const Table<NORM> table((float*)(lds + (GRAIN ? kWaves * kAtOnce * kStage : 0)), a);
+    const Table<NORM> table((float*)(lds + (GRAIN ? kWaves * kAtOnce * kStage : 0) + (NORM ? kWaves * a.sum_bytes : 0)), a);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int pieces = a.head_dim / 8, rows_at_once = 64 / pieces;
     const int row_in = (int)((unsigned)lane / (unsigned)pieces), piece = lane - row_in * pieces;
@@ -136,6 +151,10 @@ __global__ __launch_bounds__(64 * kWaves) void rotary_axes(RotaryAxesArgs a) {
 #pragma unroll
         for (int i = 0; i < kReads; ++i) partner[i] = (lane - piece) * 16 + 2 * partner_of(a, 8 * piece + i * GRAIN);
     const float per_channel = 1.0f / a.head_dim;
+    float* const sums_at = (float*)(lds + (GRAIN ? kWaves * kAtOnce * kStage : 0) + wave * a.sum_bytes);
+    const RowSums row_sums(sums_at, rows_at_once, pieces, active ? row_in : 0, piece);
+    if (NORM)
+        for (int i = lane; i < a.sum_bytes / 4; i += 64) sums_at[i] = 0;
 
     for (long block = blockIdx.x; block < a.blocks; block += gridDim.x) {
         const long group = a.head_blocks == 1 ? block : block / a.head_blocks;
@@ -152,7 +171,7 @@ __global__ __launch_bounds__(64 * kWaves) void rotary_axes(RotaryAxesArgs a) {
         // A row's token and head, or a token of -1.
         auto row_of = [&](int turn, const Side& s, int& t, int& h) {
             const int row = (turn - (s.which ? q_turns : 0)) * rows_at_once + row_in;
-            t = a.tokens_each == 1 ? 0 : (int)((unsigned)row * (unsigned)s.per_head >> 22);
+            t = a.tokens_each == 1 ? 0 : (int)((unsigned)row * (unsigned)s.per_head >> 24);
             h = row - t * s.heads;
             if (!active || turn >= turns || row >= tokens * s.heads) t = -1;
             h += s.head0;
@@ -196,7 +215,7 @@ __global__ __launch_bounds__(64 * kWaves) void rotary_axes(RotaryAxesArgs a) {
                             TYPE::unpack((unsigned)raw[u][e], x0, x1);
                             mean[u] += x0 + x1;
                         }
-                    row_sums(mean, pieces, piece, lane);
+                    row_sums(mean, active);
 #pragma unroll
                     for (int u = 0; u < kAtOnce; ++u) mean[u] *= per_channel;
                 }
@@ -212,9 +231,9 @@ __global__ __launch_bounds__(64 * kWaves) void rotary_axes(RotaryAxesArgs a) {
                         r[u] = __builtin_fmaf(x1, x1, r[u]);
                     }
                 }
-                row_sums(r, pieces, piece, lane);
+                row_sums(r, active);
 #pragma unroll
-                for (int u = 0; u < kAtOnce; ++u) r[u] = 1.0f / sqrtf(r[u] * per_channel + a.eps);
+                for (int u = 0; u < kAtOnce; ++u) r[u] = __builtin_amdgcn_rsqf(__builtin_fmaf(r[u], per_channel, a.eps));      // (good to a unit of 2^-23)
             }
 #pragma unroll
             for (int u = 0; u < kAtOnce; ++u) {
@@ -300,35 +319,36 @@ hipError_t launch_rotary_axes(RotaryAxesArgs a, int dtype, hipStream_t stream) {
     const int grain = a.pairing == VQ_PAIRS_NEIGHBOURS || a.axes == 0 ? 0 : all % 8 == 0 ? 8 : all & -all;
     a.has_bias = a.norm && (a.bias[0] || a.bias[1]);
     const int pieces = a.head_dim / 8, rows_at_once = 64 / pieces, heads = a.q_heads + a.k_heads;
-    // A workgroup's rows: a turn of its wavefronts each, or as many tokens as fill up to kMostTurns of them best, where the chip is full
-    // several times over with them.
-    const long rows = (long)a.T * heads / 2048;
+    a.sum_bytes = a.norm ? kAtOnce * rows_at_once * ((pieces + 3) / 4) * 16 : 0;
+    auto lds_of = [&](int tokens) {
+        return (size_t)kWaves * a.sum_bytes + (grain ? kWaves * kAtOnce * kStage : 0) + (size_t)tokens * a.head_dim * 4 * (a.norm ? (a.has_bias ? 6 : 4) : 2);
+    };
     a.tokens_each = 1;
     a.heads_each = heads;
-    if (rows < heads) {
-        const long least = (long)kWaves * rows_at_once;
-        a.heads_each = (int)(rows > least ? (rows + least - 1) / least * least : least);
-        if (a.heads_each > kMaxHeads) a.heads_each = kMaxHeads / (int)least * (int)least;
-        if (a.heads_each > heads) a.heads_each = heads;
+    if (a.T < kResident / 2) {
+        // Few tokens: their heads are dealt to workgroups, a turn of its wavefronts each if there are workgroups enough.
+        const int turns = (heads + kWaves * rows_at_once - 1) / (kWaves * rows_at_once), most = kResident / a.T, blocks = turns < most ? turns : most;
+        a.heads_each = (heads + blocks - 1) / blocks;
     } else {
-        double best = 0;
-        for (int n = 1; n <= kMaxTokens && (n == 1 || (long)n * heads <= rows); ++n) {
+        // As many tokens a workgroup as cost least: turns of its wavefronts, and what its table takes, about four of them, for every time that
+        // the chip is filled.  7257 tokens, 20 + 4 heads of 96 with mean, variance and biases: 26 us with three tokens, XX with five.
+        double least = 0;
+        for (int n = 1; n <= kMaxTokens && (n == 1 || lds_of(n) <= kLds); ++n) {
             const int turns = (n * a.q_heads + rows_at_once - 1) / rows_at_once + (n * a.k_heads + rows_at_once - 1) / rows_at_once;
+            if (n > 1 && turns > 8 * kWaves * kAtOnce) break;
             const int each = (turns + kWaves * kAtOnce - 1) / (kWaves * kAtOnce) * kAtOnce;
-            if (n > 1 && each > kMostTurns) break;
-            const double full = (double)n * heads / (each * kWaves * rows_at_once);
-            if (full > best * 0.999) best = full, a.tokens_each = n;
+            const double filled = ((a.T + n - 1) / n) / (double)kResident, cost = (filled <= 1 ? 1 : filled + 0.5) * (each + 4);
+            if (n == 1 || cost < least) least = cost, a.tokens_each = n;
         }
     }
     a.head_blocks = (heads + a.heads_each - 1) / a.heads_each;
     a.blocks = (((long)a.T + a.tokens_each - 1) / a.tokens_each) * a.head_blocks;
-    // (row * per_head >> 22 is row / heads: several tokens are at most 2^11 rows of 2^10 heads)
-    a.per_head[0] = ((1 << 22) + a.q_heads - 1) / a.q_heads;
-    a.per_head[1] = a.k_heads ? ((1 << 22) + a.k_heads - 1) / a.k_heads : 0;
+    // (row * per_head >> 24 is row / heads: several tokens are at most 2^12 rows of 2^11 heads)
+    a.per_head[0] = ((1 << 24) + a.q_heads - 1) / a.q_heads;
+    a.per_head[1] = a.k_heads ? ((1 << 24) + a.k_heads - 1) / a.k_heads : 0;
     auto extent = [&](int64_t token, int64_t head, int heads) { return 2 * ((a.tokens_each - 1) * token + (heads - 1) * head + a.head_dim); };
     bool wide = extent(a.q_token, a.q_head, a.q_heads) >= 1l << 31 || extent(a.qo_token, a.qo_head, a.q_heads) >= 1l << 31;
     if (a.k_heads) wide = wide || extent(a.k_token, a.k_head, a.k_heads) >= 1l << 31 || extent(a.ko_token, a.ko_head, a.k_heads) >= 1l << 31;
-    const size_t lds = (grain ? kWaves * kAtOnce * kStage : 0) + (size_t)a.tokens_each * a.head_dim * 4 * (a.norm ? (a.has_bias ? 6 : 4) : 2);
     void (*kernel)(RotaryAxesArgs) = nullptr;
     const bool f16 = dtype == VQ_F16;
     switch (a.norm) {
@@ -336,7 +356,7 @@ hipError_t launch_rotary_axes(RotaryAxesArgs a, int dtype, hipStream_t stream) {
         case 1 + VQ_NORM_RMS: kernel = f16 ? kernel_of<F16, 1 + VQ_NORM_RMS>(grain, wide) : kernel_of<BF16, 1 + VQ_NORM_RMS>(grain, wide); break;
         default: kernel = f16 ? kernel_of<F16, 1 + VQ_NORM_LAYER>(grain, wide) : kernel_of<BF16, 1 + VQ_NORM_LAYER>(grain, wide); break;
     }
-    return enqueue(kernel, dim3((unsigned)(a.blocks < 1 << 20 ? a.blocks : 1 << 20)), dim3(64 * kWaves), stream, a, lds);
+    return enqueue(kernel, dim3((unsigned)(a.blocks < 1 << 20 ? a.blocks : 1 << 20)), dim3(64 * kWaves), stream, a, lds_of(a.tokens_each));
 }
 
 }  // namespace vq

@@ -61,7 +61,7 @@ def test_rotary_refusals(lib, norm):
     if norm is None:
         assert r(axes=0) == SHAPE
     else:
-        assert [r(n=2), r(n=-1), r(eps=0.0), r(eps=-1.0), r(eps=math.nan), r(eps=math.inf)] == [SHAPE] * 6
+        assert [r(n=2), r(n=-1), r(eps=0.0), r(eps=-1.0), r(eps=math.nan), r(eps=math.inf), r(eps=1e-31)] == [SHAPE] * 7
         assert [r(w=tuple(A + 4 if i == j else A for j in range(4))) for i in range(4)] == [ALIGN] * 4
         assert [r(axes=0, sec=None, p=None, f=None, amp=math.nan, pair=9), r(w=(A,) * 4), r(hk=0, k=None, ko=None, w=(A, A, A + 4, None))] == [ARCH] * 3
 
