@@ -138,6 +138,7 @@ template <class ARGS, class T, int N>
 struct Keys {
     static constexpr bool kFirstSeen = true;       // a row that sees any key sees the first of its first tile
     static constexpr bool kTwoTensors = false;
+    static constexpr bool kStretches = false;      // of keys that a row sees: one, or several (seen())
     struct Row {                                   // what one row sees
         int visible;
         __device__ __forceinline__ Row(const ARGS& a, const Span& s, int token) : visible(keys_seen(a, s, token)) {}
@@ -166,6 +167,7 @@ template <class T, int N>
 struct Keys<AttentionWindowArgs, T, N> {
     static constexpr bool kFirstSeen = false;
     static constexpr bool kTwoTensors = false;
+    static constexpr bool kStretches = true;
     struct Row {
         int lo, size, sinks;                       // the window's first key, how many it has, first keys
         __device__ __forceinline__ Row(const AttentionWindowArgs& a, const Span& s, int token) {
@@ -208,12 +210,15 @@ struct Keys<AttentionWindowArgs, T, N> {
         const int key = key_of_tile(t);
         return (key >= r.lo && key + N <= r.hi) || key + N <= r.sinks;
     }
-    // (the first ones' last tile has no keys behind them, whatever the window)
-    __device__ __forceinline__ Row within(Row r, int t) const {
-        if (t < first_tiles) r.size = 0;
-        return r;
+    // A bit for every key of a tile that a row sees, N of them.  (Two instructions a score that it hides or leaves; compared one by one with
+    // three limits it takes seven.)
+    __device__ __forceinline__ uint64_t seen(const Row& r, int t) const {
+        const int key = key_of_tile(t);
+        auto ones = [](int n) { return n >= 64 ? ~0ull : (1ull << max(n, 0)) - 1; };
+        // (the first ones' last tile has no keys behind them, whatever the window)
+        const uint64_t window = t < first_tiles ? 0 : ones(r.lo + r.size - key) & ~ones(r.lo - key);
+        return window | ones(r.sinks - key);
     }
-    __device__ __forceinline__ bool sees(const Row& r, int key) const { return (unsigned)(key - r.lo) < (unsigned)r.size || key < r.sinks; }
 };
 
 // Keys that all sequences share, then the sequence's own as in the first.
@@ -221,6 +226,7 @@ template <class T, int N>
 struct Keys<AttentionPrefixArgs, T, N> {
     static constexpr bool kFirstSeen = true;
     static constexpr bool kTwoTensors = true;
+    static constexpr bool kStretches = false;
     struct Row {
         int visible;                               // of its own
         __device__ __forceinline__ Row(const AttentionPrefixArgs& a, const Span& s, int token) : visible(keys_seen(a, s, token)) {}
@@ -349,6 +355,12 @@ struct ValueReader {
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
 };
+
+// A score whose bit `at` of `seen` is set, else -inf.
+__device__ __forceinline__ float seen_or_hidden(float score, unsigned seen, int at) {
+    const int m = (int)(seen << (31 - at)) >> 31;
+    return __builtin_bit_cast(float, (__builtin_bit_cast(int, score) & m) | ((int)0xFF800000 & ~m));
+}
 
 // The key of register r of a block of S^T, less the block's first.
 __device__ __forceinline__ constexpr int key_of(int r) { return (r & 3) + 8 * (r >> 2); }   // + 4 (lane / 32)

@@ -123,13 +123,22 @@ __device__ __forceinline__ void rows_of(const ARGS& a, unsigned block, char* lds
             v16f sc = {};
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) sc = mfma<TYPE>(k_read.read(at, 0, i), q[i], sc);
-            const int first = keys.key_of_tile(t) + 4 * half;
-            const typename KeysOf::Row here = keys.within(sight, t);
             float top = -kInf;
+            if constexpr (KeysOf::kStretches) {
+                const unsigned seen = (unsigned)(keys.seen(sight, t) >> (4 * half));
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                sc[i] = keys.sees(here, first + key_of(i)) ? sc[i] * a.scale_log2 : -kInf;
-                top = fmaxf(top, sc[i]);
+                for (int i = 0; i < 16; ++i) {
+                    sc[i] = seen_or_hidden(sc[i] * a.scale_log2, seen, key_of(i));
+                    top = fmaxf(top, sc[i]);
+                }
+            } else {
+                const int first = keys.key_of_tile(t) + 4 * half;
+                const typename KeysOf::Row here = keys.within(sight, t);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    sc[i] = keys.sees(here, first + key_of(i)) ? sc[i] * a.scale_log2 : -kInf;
+                    top = fmaxf(top, sc[i]);
+                }
             }
             top = fmaxf(top, other_half(top));
             const float up = fmaxf(m, top);

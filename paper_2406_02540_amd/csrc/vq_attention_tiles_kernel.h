@@ -114,11 +114,22 @@ __device__ __forceinline__ void tiles_of(const ARGS& a, unsigned block, char* ld
     v16f sc[2];
     const KeyReader<CHUNKS, STEPS> k_read((lds_bytes)lds, lane);
     const ValueReader<CHUNKS> v_read((lds_bytes)lds + 2 * kTile, lane);
-    auto hide = [&](int t, int j) {
-        const int first = keys.key_of_tile(t) + 32 * j + 4 * half;
-        const typename KeysOf::Row here = keys.within(sight, t);
+    auto hide = [&](int t) {
+        if constexpr (KeysOf::kStretches) {
+            const uint64_t seen = keys.seen(sight, t) >> (4 * half);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[j][i] = keys.sees(here, first + key_of(i)) ? sc[j][i] : -kInf;
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[j][i] = seen_or_hidden(sc[j][i], (unsigned)(seen >> (32 * j)), key_of(i));
+        } else {
+            const typename KeysOf::Row here = keys.within(sight, t);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int first = keys.key_of_tile(t) + 32 * j + 4 * half;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[j][i] = keys.sees(here, first + key_of(i)) ? sc[j][i] : -kInf;
+            }
+        }
     };
     auto relative = [&](int j) {
         float top = -kInf;
@@ -165,8 +176,7 @@ __device__ __forceinline__ void tiles_of(const ARGS& a, unsigned block, char* ld
         const int buffer = (t - t0) & 1;
         constexpr bool MORE = decltype(more)::value;
         if (!keys.whole(seen_by_all, t)) {
-            hide(t, 0);
-            hide(t, 1);
+            hide(t);
             top = -kInf;
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[0][i]);
@@ -214,8 +224,8 @@ __device__ __forceinline__ void tiles_of(const ARGS& a, unsigned block, char* ld
             sc[j] = v16f{};
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) sc[j] = mfma<TYPE>(k_read.read(0, 32 * j, i), q[i], sc[j]);
-            hide(t0, j);
         }
+        hide(t0);
         // the reference is the first tile's largest score (a row that sees any key sees the first of its first tile)
         top = -kInf;
 #pragma unroll

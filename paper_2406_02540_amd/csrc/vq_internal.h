@@ -133,7 +133,7 @@ struct RotaryAxesArgs {
     int pairing, axes, pairs, sections[VQ_MAX_AXES];
     int T, q_heads, k_heads, head_dim;
     int64_t q_token, q_head, qo_token, qo_head, k_token, k_head, ko_token, ko_head;   // strides in elements
-    int has_bias, sum_bytes, tokens_each, heads_each, head_blocks, per_head[2];       // the launch's: of a workgroup,
+    int has_bias, tokens_each, heads_each, head_blocks, per_head[2];                  // the launch's: of a workgroup,
     int64_t blocks;                                                                   // and what workgroups take in turn
 };
 hipError_t launch_rotary_axes(RotaryAxesArgs a, int dtype, hipStream_t stream);

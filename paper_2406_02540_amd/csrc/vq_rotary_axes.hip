@@ -93,32 +93,18 @@ __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// Sums over the lanes of a row, kAtOnce of them: every lane writes its own and reads its row's, four a read, the places behind the last zero.
-// (Through LDS the row's lanes are two ways apart; by exchanges, of which nine lanes take five one behind the other, it took 74 us
-// instead of XX at 32768 tokens, 16 + 16 heads of 72.)
-struct RowSums {
-    float* const mine;
-    const float* const row;
-    const int quads, next;          // floats from one sum's to the next one's
-    __device__ __forceinline__ RowSums(float* at, int rows, int pieces, int row_in, int piece)
-        : mine(at + row_in * (4 * ((pieces + 3) / 4)) + piece), row(at + row_in * (4 * ((pieces + 3) / 4))), quads((pieces + 3) / 4), next(rows * 4 * ((pieces + 3) / 4)) {}
-    __device__ __forceinline__ void operator()(float (&v)[kAtOnce], bool active) const {
-        if (active)
+// The sums over a row's lanes, `pieces` of them from lane - piece on.  (Through LDS, four lanes a read, it takes as long.)
+__device__ __forceinline__ void row_sums(float (&v)[kAtOnce], int pieces, int piece, int lane) {
+    for (int i = 1; i < pieces; i *= 2) {
+        float o[kAtOnce];
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) mine[u * next] = v[u];
-        wave_fence();
-        v4f s[kAtOnce];
+        for (int n = 0; n < kAtOnce; ++n) o[n] = __shfl_down(v[n], i);
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) s[u] = active ? *(const v4f*)(row + u * next) : v4f{0, 0, 0, 0};
-        for (int i = 1; i < quads; ++i)
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u)
-                if (active) s[u] += *(const v4f*)(row + u * next + 4 * i);
-        wave_fence();
-#pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) v[u] = (s[u][0] + s[u][1]) + (s[u][2] + s[u][3]);
+        for (int n = 0; n < kAtOnce; ++n) v[n] += piece + i < pieces ? o[n] : 0.0f;
     }
-};
+#pragma unroll
+    for (int n = 0; n < kAtOnce; ++n) v[n] = __shfl(v[n], lane - piece);
+}
 
 // What a turn of a wavefront works on: rows of q or of k, all the same for its lanes.
 struct Side {
@@ -139,7 +125,7 @@ __global__ __launch_bounds__(64 * kWaves, WIDE || GRAIN == 1 ? 5 : 6) void rotar
     typedef typename TYPE::T T;
     typedef typename std::conditional<WIDE, int64_t, unsigned>::type Offset;
     extern __shared__ __align__(16) char lds[];
-    const Table<NORM> table((float*)(lds + (GRAIN ? kWaves * kAtOnce * kStage : 0) + (NORM ? kWaves * a.sum_bytes : 0)), a);
+    const Table<NORM> table((float*)(lds + (GRAIN ? kWaves * kAtOnce * kStage : 0)), a);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int pieces = a.head_dim / 8, rows_at_once = 64 / pieces;
     const int row_in = (int)((unsigned)lane / (unsigned)pieces), piece = lane - row_in * pieces;
@@ -151,10 +137,6 @@ __global__ __launch_bounds__(64 * kWaves, WIDE || GRAIN == 1 ? 5 : 6) void rotar
 #pragma unroll
         for (int i = 0; i < kReads; ++i) partner[i] = (lane - piece) * 16 + 2 * partner_of(a, 8 * piece + i * GRAIN);
     const float per_channel = 1.0f / a.head_dim;
-    float* const sums_at = (float*)(lds + (GRAIN ? kWaves * kAtOnce * kStage : 0) + wave * a.sum_bytes);
-    const RowSums row_sums(sums_at, rows_at_once, pieces, active ? row_in : 0, piece);
-    if (NORM)
-        for (int i = lane; i < a.sum_bytes / 4; i += 64) sums_at[i] = 0;
 
     for (long block = blockIdx.x; block < a.blocks; block += gridDim.x) {
         const long group = a.head_blocks == 1 ? block : block / a.head_blocks;
@@ -215,7 +197,7 @@ __global__ __launch_bounds__(64 * kWaves, WIDE || GRAIN == 1 ? 5 : 6) void rotar
                             TYPE::unpack((unsigned)raw[u][e], x0, x1);
                             mean[u] += x0 + x1;
                         }
-                    row_sums(mean, active);
+                    row_sums(mean, pieces, piece, lane);
 #pragma unroll
                     for (int u = 0; u < kAtOnce; ++u) mean[u] *= per_channel;
                 }
@@ -231,7 +213,7 @@ __global__ __launch_bounds__(64 * kWaves, WIDE || GRAIN == 1 ? 5 : 6) void rotar
                         r[u] = __builtin_fmaf(x1, x1, r[u]);
                     }
                 }
-                row_sums(r, active);
+                row_sums(r, pieces, piece, lane);
 #pragma unroll
                 for (int u = 0; u < kAtOnce; ++u) r[u] = __builtin_amdgcn_rsqf(__builtin_fmaf(r[u], per_channel, a.eps));      // (good to a unit of 2^-23)
             }
@@ -319,9 +301,8 @@ hipError_t launch_rotary_axes(RotaryAxesArgs a, int dtype, hipStream_t stream) {
     const int grain = a.pairing == VQ_PAIRS_NEIGHBOURS || a.axes == 0 ? 0 : all % 8 == 0 ? 8 : all & -all;
     a.has_bias = a.norm && (a.bias[0] || a.bias[1]);
     const int pieces = a.head_dim / 8, rows_at_once = 64 / pieces, heads = a.q_heads + a.k_heads;
-    a.sum_bytes = a.norm ? kAtOnce * rows_at_once * ((pieces + 3) / 4) * 16 : 0;
     auto lds_of = [&](int tokens) {
-        return (size_t)kWaves * a.sum_bytes + (grain ? kWaves * kAtOnce * kStage : 0) + (size_t)tokens * a.head_dim * 4 * (a.norm ? (a.has_bias ? 6 : 4) : 2);
+        return (size_t)(grain ? kWaves * kAtOnce * kStage : 0) + (size_t)tokens * a.head_dim * 4 * (a.norm ? (a.has_bias ? 6 : 4) : 2);
     };
     a.tokens_each = 1;
     a.heads_each = heads;
@@ -331,7 +312,7 @@ hipError_t launch_rotary_axes(RotaryAxesArgs a, int dtype, hipStream_t stream) {
         a.heads_each = (heads + blocks - 1) / blocks;
     } else {
         // As many tokens a workgroup as cost least: turns of its wavefronts, and what its table takes, about four of them, for every time that
-        // the chip is filled.  7257 tokens, 20 + 4 heads of 96 with mean, variance and biases: 26 us with three tokens, XX with five.
+        // the chip is filled.  7257 tokens, 20 + 4 heads of 96 with mean, variance and biases: 33 us with three tokens, 24 with five.
         double least = 0;
         for (int n = 1; n <= kMaxTokens && (n == 1 || lds_of(n) <= kLds); ++n) {
             const int turns = (n * a.q_heads + rows_at_once - 1) / rows_at_once + (n * a.k_heads + rows_at_once - 1) / rows_at_once;
