@@ -77,12 +77,11 @@ __device__ __forceinline__ void rows_of(const ARGS& a, unsigned block, char* lds
         const int t0 = split_begin(a, keys.tiles, split), t1 = split_begin(a, keys.tiles, split + 1);
 
         bool own = true;            // whether the loaders are those of the sequence's own keys
-        if constexpr (KeysOf::kTwoTensors)
-            if (t0 + wave < keys.first_tiles) {
-                own = false;
-                k_load = LoaderK((int)(2 * a.pk_token), head_bytes, lane);
-                v_load = LoaderV((int)(2 * a.pv_token), head_bytes, lane);
-            }
+        if constexpr (KeysOf::kTwoTensors) {
+            own = t0 + wave >= keys.first_tiles;      // (another block of rows may have left the others)
+            k_load = LoaderK((int)(2 * (own ? a.k_token : a.pk_token)), head_bytes, lane);
+            v_load = LoaderV((int)(2 * (own ? a.v_token : a.pv_token)), head_bytes, lane);
+        }
         auto ask = [&](int t, int to) {
             if constexpr (KeysOf::kTwoTensors)
                 if (!own && t >= keys.first_tiles) {

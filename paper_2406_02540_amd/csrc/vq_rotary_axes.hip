@@ -122,7 +122,6 @@ struct Side {
 // at once, four workgroups a CU, 58, 67 and 82; one row, seven a CU, 52, 59 and 70 (inputs that are not in the caches).
 template <class TYPE, int GRAIN, int NORM, bool WIDE>
 __global__ __launch_bounds__(64 * kWaves, WIDE || GRAIN == 1 ? 5 : 6) void rotary_axes(RotaryAxesArgs a) {
-    typedef typename TYPE::T T;
     typedef typename std::conditional<WIDE, int64_t, unsigned>::type Offset;
     extern __shared__ __align__(16) char lds[];
     const Table<NORM> table((float*)(lds + (GRAIN ? kWaves * kAtOnce * kStage : 0)), a);
@@ -318,7 +317,7 @@ hipError_t launch_rotary_axes(RotaryAxesArgs a, int dtype, hipStream_t stream) {
             const int turns = (n * a.q_heads + rows_at_once - 1) / rows_at_once + (n * a.k_heads + rows_at_once - 1) / rows_at_once;
             if (n > 1 && turns > 8 * kWaves * kAtOnce) break;
             const int each = (turns + kWaves * kAtOnce - 1) / (kWaves * kAtOnce) * kAtOnce;
-            const double filled = ((a.T + n - 1) / n) / (double)kResident, cost = (filled <= 1 ? 1 : filled + 0.5) * (each + 4);
+            const double filled = (double)(((long)a.T + n - 1) / n) / kResident, cost = (filled <= 1 ? 1 : filled + 0.5) * (each + 4);
             if (n == 1 || cost < least) least = cost, a.tokens_each = n;
         }
     }

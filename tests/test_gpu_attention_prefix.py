@@ -87,6 +87,14 @@ def test_a_prompt_among_single_tokens():
     _run([1] * 30 + [333] + [1] * 30, [5] * 61, 77, 2, 2, 72, BF16, False)
 
 
+def test_blocks_of_rows_that_begin_in_the_prefix_and_behind_it():
+    # one sequence of several blocks of rows among single tokens, its keys divided: later blocks see more keys, so that a workgroup's part begins in
+    # the prefix for one block and behind it for the next, and k, v lie otherwise than the prefix
+    for lq, lk in (([1000] + [1] * 32, [1000] + [9] * 32), ([1] * 33 + [1020], [3] * 33 + [1100])):
+        _run(lq, lk, 600, 1, 1, 64, F16, True)
+        _run(lq, lk, 600, 1, 1, 72, BF16, True, before=1, behind=2)
+
+
 def test_no_own_keys_and_no_prefix():
     for n in (2, 300):
         q = torch.randn(n, 4, 72, device="cuda").to(F16)
