@@ -16,7 +16,8 @@ AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix,
     if (rows > 64l * sequences || again < 8l << 20) {
         c.pass = rows > 32l * sequences ? kAttentionTiles : kAttentionRows;
         const long keys = (long)Tk / sequences + prefix, tiles = c.pass == kAttentionTiles ? attention_items(sequences, Tq, group) : sequences;
-        while (c.split_shift < 6 && (tiles * kv_heads << c.split_shift) < (c.pass == kAttentionTiles ? 512 : 2048) && keys >> (c.split_shift + 1) >= 256) ++c.split_shift;
+        if (c.pass == kAttentionRows) c.split_shift = split_of_equal(tiles * kv_heads, keys);
+        while (c.pass == kAttentionTiles && c.split_shift < 6 && (tiles * kv_heads << c.split_shift) < 512 && keys >> (c.split_shift + 1) >= 256) ++c.split_shift;
         c.fits = groups(tiles, c.split_shift) * 256 < 1l << 32;
         return c;
     }

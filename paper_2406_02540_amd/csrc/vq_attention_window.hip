@@ -12,14 +12,14 @@ long keys_in_window(int sequences, int Tq, int Tk, int group, int causal, int le
     return keys < all ? keys : all;
 }
 
-// As choose_attention(), with the keys that a block of rows works on in the place of the sequence's.
+// As choose_attention(), with the keys that a block of rows works on in the place of the sequence's: a window makes them equal.
 AttentionChoice choose_attention_window(int sequences, int Tq, int Tk, int heads, int kv_heads, int causal, int left, int right, int sinks) {
     const int group = heads / kv_heads;
     const long keys = keys_in_window(sequences, Tq, Tk, group, causal, left, right, sinks);
     const bool rows = (long)Tq * group <= 32l * sequences;
     const long tiles = rows ? (long)sequences : attention_items(sequences, Tq, group), items = tiles * kv_heads;
-    int shift = 0;
-    while (shift < 6 && (items << shift) < (rows ? 2048 : 512) && keys >> (shift + 1) >= 256) ++shift;
+    int shift = rows ? split_of_equal(items, keys) : 0;
+    while (!rows && shift < 6 && (items << shift) < 512 && keys >> (shift + 1) >= 256) ++shift;
     const bool alone = rows && shift == 0 && keys <= 64 && (long)sequences * kv_heads >= 2048;
     const long most = ((tiles << shift) + kItemsRounded) * kv_heads;
     return {!rows ? kAttentionTiles : alone ? kAttentionRowsAlone : kAttentionRows, shift, most * (alone ? 64 : 256) < 1l << 32};
