@@ -428,15 +428,18 @@ size_t vq_attention_workspace_bytes(int sequences, int Tq, int Tk, int heads, in
  *
  * vq_attention_window: vq_attention in a sliding window.  With n queries and m keys query i of a sequence stands at
  *   p = i + m - n.  It sees the keys p - left .. p + right and the sequence's first `sinks` keys, of both none behind p
- *   if causal.  left, right: 0 or more, or -1 for no limit (right is not looked at if causal, but for its range); sinks >= 0.  A query that sees
- *   no key gets zeros.  What a query does not see does not reach it, finite or not, but for a value of v that is not finite in a
- *   block of 128 query rows (query heads of a head of k, then tokens) some of which see it.
+ *   if causal.  left, right: 0 or more, or -1 for no limit (right is not looked at if causal, but for its range); sinks >= 0.
+ *   A query that sees no key gets zeros.  Keys that no query row of a block of 128 (the query heads of a head of k, then tokens) sees are
+ *   not read, and may hold anything; so may the key, but not the value, of one that others of the block see.
  *
  * vq_attention_prefix: vq_attention of sequences whose first keys are the same ones, given once: every query sees all of
  *   prefix_k, prefix_v [prefix, kv_heads, head_dim], and its own sequence's keys behind them as vq_attention has it
  *   (causal: its keys 0 .. i + m - n).  prefix >= 0, prefix + Tk at most 2^31 - 256; a query with neither gets zeros.
  *     strides    host, twelve of them: token and head of q, prefix_k, prefix_v, k, v, out
  *   Few queries a sequence: the prefix is read once for all of them, and not once for every sequence.
+ *
+ * The limits on sizes and the workspace are vq_attention's, for either (a launch of the windows is rounded up by 64 sequences);
+ * two calls that may overlap in time need a workspace each.
  */
 #define VQ_MAX_AXES 4
 typedef enum vq_pairs { VQ_PAIRS_HALVES = 0, VQ_PAIRS_NEIGHBOURS = 1, VQ_PAIRS_AXIS_HALVES = 2 } vq_pairs;

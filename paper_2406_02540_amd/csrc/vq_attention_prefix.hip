@@ -1,6 +1,11 @@
 // Attention of sequences behind keys that all of them share.  In one pass, the shared keys first, by tiles of query rows or by rows; or, where a
 // sequence has few rows and the shared keys are many, in parts: all sequences' rows together with the shared keys, which so are read once for
 // all, and in the same launch each sequence's with its own, then a join.
+//
+// One pass by tiles is bound as vq_attention's: 6 images of 4096 tokens behind 300, 16 heads of 72, 615 us (810 TFLOP/s; matrix units busy 51 % of the cycles
+// at 1.6 GHz).  In parts: 64 single tokens behind 8192 keys and up to 700 of their own, 32 heads on 8 of 128, 36 us (99 MB, 19 us at a copy's rate): 31 for the
+// parts, of which the shared keys alone take 26 (two tiles of 128 rows a head) and the own ones 19 (a few tiles of keys a workgroup: waits for first loads), 5 for the join;
+// as a part of every sequence's own keys they are 2.2 GB.  In two launches, one behind the other, it took 54.
 #include "vq_attention_rows_kernel.h"
 #include "vq_attention_tiles_kernel.h"
 
@@ -11,19 +16,24 @@ AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix,
     const long rows = (long)Tq * group;          // of all sequences
     AttentionPrefixChoice c{};
     auto groups = [&](long tiles, int shift) { return ((tiles << shift) + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds * kv_heads; };
-    // What one pass reads of the shared keys more than once.
-    const long again = (long)(sequences - 1) * prefix * kv_heads * head_dim * 4;
-    if (rows > 64l * sequences || again < 8l << 20) {
+    // In parts where one pass would read at least 8 MB of shared keys over and over, and a sequence's rows leave tiles of 128 as empty as the parts'
+    // own traffic weighs.  Parts and one pass (us; heads on heads of k and v): 8 single tokens behind 4096 keys, 32 on 8 of 128, 15 and 26; 16 behind 512
+    // 13.3 and 16.3; 2 behind 8192 17.7 and 19.0; 3 x 4 behind 4096, 16 on 2 of 64 (4 MB), 12.6 and 12.1; 12 x 30 behind 3000, 16 on 8 of 64, 25 and 41, x 64 37 and
+    // 47; 64 x 100 behind 4000, 8 of 128, 153 and 208; 200 x 64 behind 1000, 16 of 72, 228 and 170.
+    const long again = (long)(sequences - 1) * prefix * kv_heads * head_dim * 4, own = (long)Tk / sequences;
+    if (again < 8l << 20 || (rows > 32l * sequences && (rows > 128l * sequences || prefix < 2048 || own > prefix / 4))) {
         c.pass = rows > 32l * sequences ? kAttentionTiles : kAttentionRows;
-        const long keys = (long)Tk / sequences + prefix, tiles = c.pass == kAttentionTiles ? attention_items(sequences, Tq, group) : sequences;
+        const long keys = own + prefix, tiles = c.pass == kAttentionTiles ? attention_items(sequences, Tq, group) : sequences;
         if (c.pass == kAttentionRows) c.split_shift = split_of_equal(tiles * kv_heads, keys);
         while (c.pass == kAttentionTiles && c.split_shift < 6 && (tiles * kv_heads << c.split_shift) < 512 && keys >> (c.split_shift + 1) >= 256) ++c.split_shift;
         c.fits = groups(tiles, c.split_shift) * 256 < 1l << 32;
         return c;
     }
     c.in_parts = true;
-    const long own = (long)Tk / sequences, own_items = (long)sequences * kv_heads;
+    const long own_items = (long)sequences * kv_heads;
     while (c.split_shift < 5 && (own_items << c.split_shift) < 512 && own >> (c.split_shift + 1) >= 256) ++c.split_shift;
+    // Parts of the shared keys for half of the chip where the sequences' own workgroups fill it by themselves: 64 single tokens behind 8192 keys
+    // with 4, 8, 16 and 32 of them 53, 37, 43 and 52 us; 5 x 7 behind 30011, where they do not, with 8, 16, 32 and 64 56, 34, 24.5 and 25.6.
     c.pass = rows <= 32 ? kAttentionRows : kAttentionTiles;
     const long tiles = c.pass == kAttentionRows ? 1 : (rows + kTileRows - 1) / kTileRows;
     while (c.shared_shift < 5 && (tiles * kv_heads << c.shared_shift) < (own_items >= 256 ? 128 : 384) && (long)prefix >> (c.shared_shift + 1) >= 256) ++c.shared_shift;
