@@ -99,6 +99,17 @@ def test_a_prompt_among_single_tokens():
     _run(lq, lk, 2, 2, 72, BF16, 128, 64, 0, False)
 
 
+def test_no_keys_at_all():
+    for n in (2, 300):
+        q = torch.randn(n, 4, 72, device="cuda").to(F16)
+        kv = torch.empty(0, 2, 72, dtype=F16, device="cuda")
+        cu = torch.tensor([0, n - 1, n - 1], dtype=torch.int32, device="cuda")
+        for args in ((5, 5, 3), (None, None, 0), (0, 0, 70)):
+            out = torch.full_like(q, 3.0)
+            vq.vq_attention_window(q, kv, kv, cu, torch.zeros(3, dtype=torch.int32, device="cuda"), *args, out=out)
+            assert (out[:n - 1] == 0).all() and (out[n - 1] == 3).all()
+
+
 def test_windows_of_the_largest_numbers():
     top = 2**31 - 1
     for lq, lk in (([300], [300]), ([1, 2], [500, 3]), ([50], [3])):
