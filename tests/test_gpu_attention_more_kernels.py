@@ -30,6 +30,7 @@ PREFIX = {
     "parts by rows": (True, ROWS, False, True, [1] * 10, _lengths(2, 10, 0, 300), 9000, 3, 3),
     "parts by rows, divided": (True, ROWS, True, True, [1] * 8, _lengths(3, 8, 800, 1500), 11000, 4, 4),
     "parts by tiles": (True, TILES, False, True, [1] * 60 + [3, 0], _lengths(4, 61, 0, 200, (700,)), 5000, 8, 2),
+    "parts by tiles, many sequences": (True, TILES, False, True, [1] * 129 + [40], _lengths(8, 130, 0, 60), 5001, 8, 2),
     "parts by tiles, whole": (True, TILES, False, False, _lengths(5, 700, 0, 3, (40,)), _lengths(6, 700, 0, 40, (100,)), 130, 8, 2),
     "parts by tiles, divided": (True, TILES, True, True, [7] * 12, _lengths(7, 12, 600, 900), 4001, 12, 2),
 }
