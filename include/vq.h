@@ -422,8 +422,8 @@ size_t vq_attention_workspace_bytes(int sequences, int Tq, int Tk, int heads, in
  *     VQ_NORM_RMS    y = x / sqrt(mean x^2 + eps) * weight + bias
  *     VQ_NORM_LAYER  y = (x - mean x) / sqrt(mean (x - mean x)^2 + eps) * weight + bias
  *   over the head_dim channels of a head, then vq_rotary_axes of y.  All in fp32, one rounding at the end.  weight and bias are
- *   fp32 [head_dim], those of q and those of k, each NULL for ones or zeros.  eps within [1e-30, 1e30].  axes = 0: the norm alone (positions,
- *   inv_freq, sections, pairing and amplitude are not looked at).  Not checked on the device: the squares of a head within
+ *   fp32 [head_dim], those of q and those of k (not looked at if k_heads is 0), each NULL for ones or zeros.  eps within [1e-30, 1e30].
+ *   axes = 0: the norm alone (positions, inv_freq, sections, pairing and amplitude are not looked at).  Not checked on the device: the squares of a head within
  *   the range of fp32; a head with a value that is not finite has no specified values, the others keep theirs.
  *
  * vq_attention_window: vq_attention in a sliding window.  With n queries and m keys query i of a sequence stands at

@@ -761,7 +761,8 @@ int vq_norm_rotary(const void* q, void* q_out, const void* k, void* k_out, int d
     vq::RotaryAxesArgs a{};
     set_views(a, q, q_out, k, k_out, T, q_heads, k_heads, head_dim, strides);
     a.norm = 1 + norm, a.eps = eps;
-    a.weight[0] = q_weight, a.weight[1] = k_weight, a.bias[0] = q_bias, a.bias[1] = k_bias;
+    a.weight[0] = q_weight, a.bias[0] = q_bias;
+    if (k_heads > 0) a.weight[1] = k_weight, a.bias[1] = k_bias;
     if (axes > 0) {
         a.positions = positions, a.inv_freq = inv_freq, a.amplitude = amplitude, a.pairing = pairing, a.axes = axes, a.pairs = pairs;
         for (int i = 0; i < axes; ++i) a.sections[i] = sections[i];

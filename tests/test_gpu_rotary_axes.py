@@ -1,8 +1,11 @@
 """Rotary positions of several axes, and norms of heads with them, against the formulas in 64 bits."""
+import ctypes
+
 import pytest
 import torch
 
 import paper_2406_02540_amd as vq
+from paper_2406_02540_amd.binding import lib
 import more_operator_util as mu
 import operator_util as ou
 
@@ -154,6 +157,20 @@ def test_no_tokens():
     p, f = torch.empty(2, 0, dtype=torch.int32, device="cuda"), torch.ones(16, device="cuda")
     assert vq.vq_rotary_axes(q, q, p, f, (8, 8))[0].shape == (0, 4, 64)
     assert vq.vq_norm_rotary(q, None)[0].shape == (0, 4, 64)
+
+
+def test_what_belongs_to_k_is_not_looked_at_without_it():
+    T, H, D = 5, 4, 64
+    buf, q, _ = _views(T, H, 1, D, F16)
+    w = torch.rand(D + 4, device="cuda") + 0.5
+    want = vq.vq_norm_rotary(q, None, w[:D])[0]
+    got = torch.empty_like(want)
+    other = ctypes.c_void_p(w.data_ptr() + 4)           # (with heads of k its weights and biases would be refused)
+    strides = (ctypes.c_int64 * 8)(*q.stride()[:2], *got.stride()[:2], 0, 0, 0, 0)
+    P, stream = ctypes.c_void_p, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert lib().vq_norm_rotary(P(q.data_ptr()), P(got.data_ptr()), None, None, 0, 0, ctypes.c_float(1e-6), P(w.data_ptr()), None, other, other, None,
+                                None, ctypes.c_float(1), 0, 0, None, T, H, 0, D, strides, stream) == 0
+    assert torch.equal(got, want)
 
 
 @pytest.mark.parametrize("T", [1, 200, 4000])
