@@ -15,8 +15,7 @@ AttentionChoice choose_attention(int sequences, int Tq, int Tk, int heads, int k
     // 442 and 170, 512 queries over 32768 584 and 280, 64 tokens of 2 sequences over 8192 156 and 35.  Eight turns are for ragged sequences,
     // where the longest decides: workgroups for two make those 16 199, but 64 equal ones over 4096 keys 190 instead of 215.
     const long tiles = rows ? (long)sequences : attention_items(sequences, Tq, group), items = tiles * kv_heads;
-    int shift = 0;
-    while (shift < 6 && (items << shift) < (rows ? 2048 : 512) && keys >> (shift + 1) >= 256) ++shift;
+    const int shift = split_for(rows ? kRaggedWorkgroups : 512, items, keys);
     // A wavefront alone, one tile of keys at a time, where the average sequence has a few tiles and there are sequences enough: 2048
     // sequences of 16, 16 heads of 72, 84 us, by four wavefronts 542, most of which have no keys.
     const bool alone = rows && shift == 0 && keys <= 64 && (long)sequences * kv_heads >= 2048;

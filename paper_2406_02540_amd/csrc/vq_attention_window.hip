@@ -11,22 +11,33 @@
 
 namespace vq {
 
-long keys_in_window(int sequences, int Tq, int Tk, int group, int causal, int left, int right, int sinks) {
-    const long all = (long)Tk / sequences, queries = ((long)Tq + sequences - 1) / sequences;
+namespace {
+// Keys that a block of rows would work on if its sequence had them.
+long window_of(int sequences, int Tq, int group, int causal, int left, int right, int sinks) {
+    if (left < 0 || (right < 0 && !causal)) return 1l << 40;      // (more than any)
+    const long queries = ((long)Tq + sequences - 1) / sequences;
     const long block = ((long)Tq * group <= 32l * sequences ? 32 : kTileRows) / group + 1;       // tokens of a block of rows
-    if (left < 0 || (right < 0 && !causal)) return all;
-    const long keys = (queries < block ? queries : block) + left + (causal ? 0 : right) + sinks;
+    return (queries < block ? queries : block) + left + (causal ? 0 : right) + sinks;
+}
+}  // namespace
+
+long keys_in_window(int sequences, int Tq, int Tk, int group, int causal, int left, int right, int sinks) {
+    const long all = (long)Tk / sequences, keys = window_of(sequences, Tq, group, causal, left, right, sinks);
     return keys < all ? keys : all;
 }
 
-// As choose_attention(), with the keys that a block of rows works on in the place of the sequence's: a window makes them equal.
+// As choose_attention(), with the keys that a block of rows works on in the place of the sequence's. A window makes sequences equal, one that is long
+// beside the average leaves them as ragged as they are. Single tokens of up to 32768 keys (12000 on average), 32 heads on 8 of 128, divided as equal
+// and as ragged ones (us): no window, 16 sequences 256 and 169, 48 570 and 456; windows of twice the average 198 and 155, 507 and 430, of one and a half
+// 154 and 137, 453 and 388, of the average 113 and 117, 337 and 316, of half of it 70 and 91, 197 and 214. Of up to 8000 (2900), 32 sequences: no
+// window 127 and 100, twice 99 and 95, one and a half 79 and 90, the average 61 and 79. 4 of up to 32768: 80 and 85, 80 and 85, 68 and 83, 53 and 76.
 AttentionChoice choose_attention_window(int sequences, int Tq, int Tk, int heads, int kv_heads, int causal, int left, int right, int sinks) {
     const int group = heads / kv_heads;
     const long keys = keys_in_window(sequences, Tq, Tk, group, causal, left, right, sinks);
     const bool rows = (long)Tq * group <= 32l * sequences;
     const long tiles = rows ? (long)sequences : attention_items(sequences, Tq, group), items = tiles * kv_heads;
-    int shift = rows ? split_of_equal(items, keys) : 0;
-    while (!rows && shift < 6 && (items << shift) < 512 && keys >> (shift + 1) >= 256) ++shift;
+    const bool equal = 2 * window_of(sequences, Tq, group, causal, left, right, sinks) < 3 * ((long)Tk / sequences);
+    const int shift = rows && equal ? split_of_equal(items, keys) : split_for(rows ? kRaggedWorkgroups : 512, items, keys);
     const bool alone = rows && shift == 0 && keys <= 64 && (long)sequences * kv_heads >= 2048;
     const long most = ((tiles << shift) + kItemsRounded) * kv_heads;
     return {!rows ? kAttentionTiles : alone ? kAttentionRowsAlone : kAttentionRows, shift, most * (alone ? 64 : 256) < 1l << 32};

@@ -1,0 +1,45 @@
+"""How keys are divided among workgroups where the sequences' own lengths decide: windows that do not shorten them and short prefixes as vq_attention does."""
+import ctypes
+import os
+
+import pytest
+
+from paper_2406_02540_amd import binding, build
+
+# sequences, queries, keys, heads, heads of k and v
+BATCHES = [(16, 16, 16 * 12000, 32, 8), (48, 48, 48 * 12362, 32, 8), (64, 64, 64 * 4096, 32, 8), (32, 32, 32 * 2870, 32, 8), (4, 9, 4 * 17651, 32, 8),
+           (16, 16, 16 * 11000, 16, 16), (2, 700, 2 * 9000, 8, 2), (100, 100, 100 * 400, 8, 8)]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    if not os.path.exists(binding.LIB_PATH):
+        build.build(verbose=False)
+
+
+def _attention(*sizes):
+    out = (ctypes.c_int * 2)()
+    binding.lib().vq_internal_attention_choice(*sizes, out)
+    return tuple(out)
+
+
+def _window(sizes, causal, left, right, sinks):
+    out = (ctypes.c_int * 2)()
+    binding.lib().vq_internal_attention_window_choice(*sizes, causal, left, right, sinks, out)
+    return tuple(out)
+
+
+@pytest.mark.parametrize("sizes", BATCHES)
+def test_windows_that_leave_the_sequences_as_they_are(sizes):
+    average = sizes[2] // sizes[0]
+    for causal, left, right, sinks in ((1, -1, 0, 0), (0, -1, -1, 0), (0, -1, 5, 4), (0, 5, -1, 0), (1, 2 * average, 0, 0), (1, 2**31 - 1, 2**31 - 1, 7),
+                                       (0, average, average, 0)):
+        assert _window(sizes, causal, left, right, sinks) == _attention(*sizes), (causal, left, right, sinks)
+
+
+def test_windows_that_make_them_equal():
+    # a workgroup a CU for the keys of a window, in 2 parts or 8 or one
+    assert _window((48, 48, 48 * 12362, 32, 8), 1, 4095, 0, 4) == (1, 1)
+    assert _window((4, 4, 4 * 17651, 32, 8), 1, 4095, 0, 4) == (1, 3)
+    assert _window((64, 64, 64 * 8192, 32, 8), 1, 4095, 0, 4) == (1, 0)
+    assert _window((32, 32, 32 * 2870, 32, 8), 1, 2870, 0, 4) == (1, 0)
