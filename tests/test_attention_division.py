@@ -43,3 +43,22 @@ def test_windows_that_make_them_equal():
     assert _window((4, 4, 4 * 17651, 32, 8), 1, 4095, 0, 4) == (1, 3)
     assert _window((64, 64, 64 * 8192, 32, 8), 1, 4095, 0, 4) == (1, 0)
     assert _window((32, 32, 32 * 2870, 32, 8), 1, 2870, 0, 4) == (1, 0)
+
+
+def _prefix(sequences, Tq, P, Tk, H, G, D):
+    out = (ctypes.c_int * 4)()
+    binding.lib().vq_internal_attention_prefix_choice(sequences, Tq, P, Tk, H, G, D, out)
+    return tuple(out)
+
+
+@pytest.mark.parametrize("sizes", BATCHES)
+def test_prefixes_that_leave_the_sequences_as_they_are(sizes):
+    sequences, Tq, Tk, H, G = sizes
+    assert _prefix(sequences, Tq, 0, Tk, H, G, 128) == (0, *_attention(*sizes), 0)
+    P = 16 if sequences < 100 else 4
+    assert _prefix(sequences, Tq, P, Tk, H, G, 128) == (0, *_attention(sequences, Tq, Tk + P * sequences, H, G), 0)
+
+
+def test_prefixes_that_are_most_of_the_keys():
+    assert _prefix(2, 2, 3000, 400, 8, 2, 64) == (0, 1, 3, 0)
+    assert _prefix(3, 6, 2000, 900, 32, 8, 64) == (0, 1, 3, 0)
