@@ -127,12 +127,14 @@ inline unsigned attention_grid(AttentionWindowArgs& a, long tiles) {
 }
 constexpr int kItemsRounded = 8 * kAttentionXcds;      // a launch's items are rounded up to a divisor of this many
 // How often `keys` are divided by rows where all items have about as many: turns of the chip, a workgroup a CU, times the keys of a part and what a
-// workgroup takes besides, about 256 keys.  Windows of 4100 keys, single tokens, 32 heads on 8 of 128: 48 sequences 143 us (undivided 158, as
+// workgroup takes besides, about 256 keys, and the join, as much again.  Windows of 4100 keys, single tokens, 32 heads on 8 of 128: 48 sequences 143 us (undivided 158, as
 // ragged ones are divided, in eight, 173), 16 54 (70, 80), 4 21 (64, 25), of 1028 keys 64 57 (57, 86); 16 x 2 tokens, 16 heads of 72 on 2050 39 (39, 67).
+// 16 single tokens on 512 keys 12.8 undivided and 14.9 in two, on 700 16.6 and 17.0, 1000 20.2 and 19.8; one on 512 11.5 and 11.7, 700 15.3 and 13.6; 48 on 600
+// 31.5 and 38.5, 1000 51 and 53.
 inline int split_of_equal(long items, long keys) {
     int best = 0;
     for (int shift = 1; shift <= 6 && keys >> shift >= 256; ++shift) {
-        auto cost = [&](int s) { return (((items << s) + 255) / 256) * ((keys >> s) + 256); };
+        auto cost = [&](int s) { return (((items << s) + 255) / 256) * ((keys >> s) + 256) + (s ? 256 : 0); };
         if (cost(shift) < cost(best)) best = shift;
     }
     return best;

@@ -45,6 +45,13 @@ def test_windows_that_make_them_equal():
     assert _window((32, 32, 32 * 2870, 32, 8), 1, 2870, 0, 4) == (1, 0)
 
 
+def test_a_division_pays_for_its_join():
+    # 512 keys in two parts take longer than undivided, 1000 do not
+    assert _window((16, 16, 16 * 8192, 32, 8), 1, 511, 0, 0) == (1, 0)
+    assert _window((48, 48, 48 * 8192, 32, 8), 1, 599, 0, 0) == (1, 0)
+    assert _window((16, 16, 16 * 8192, 32, 8), 1, 999, 0, 0) == (1, 1)
+
+
 def _prefix(sequences, Tq, P, Tk, H, G, D):
     out = (ctypes.c_int * 4)()
     binding.lib().vq_internal_attention_prefix_choice(sequences, Tq, P, Tk, H, G, D, out)
