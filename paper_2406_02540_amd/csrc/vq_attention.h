@@ -140,9 +140,9 @@ inline int split_of_equal(long items, long keys) {
     return best;
 }
 // And where their lengths are anything: parts of at least 256 keys of the average sequence, for that many workgroups.
-inline int split_for(long workgroups, long items, long keys) {
+inline int split_for(long workgroups, long items, long keys, int most = 6) {
     int shift = 0;
-    while (shift < 6 && (items << shift) < workgroups && keys >> (shift + 1) >= 256) ++shift;
+    while (shift < most && (items << shift) < workgroups && keys >> (shift + 1) >= 256) ++shift;
     return shift;
 }
 constexpr long kRaggedWorkgroups = 2048;     // eight turns of the chip, by rows: the longest sequence decides (figures at choose_attention)

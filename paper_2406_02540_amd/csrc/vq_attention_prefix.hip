@@ -33,7 +33,10 @@ AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix,
     }
     c.in_parts = true;
     const long own_items = (long)sequences * kv_heads;
-    while (c.split_shift < 5 && (own_items << c.split_shift) < 512 && own >> (c.split_shift + 1) >= 256) ++c.split_shift;
+    // Own keys of few rows are divided as vq_attention's (at most 32 parts of them and 32 of the shared ones): single tokens of up to 32768 keys, 12000 on
+    // average, 32 heads on 8 of 128, behind 4096 others with workgroups for two turns of the chip and for eight, 16 sequences 237 us and 182, 48 583 and 481;
+    // 32 of up to 8000 behind 2048 110 and 91; 8 equal ones of 16000 behind 8192 114 and 117, 64 of 4096 220 and 224.
+    c.split_shift = split_for(rows <= 32l * sequences ? kRaggedWorkgroups : 512, own_items, own, 5);
     // Parts of the shared keys for half of the chip where the sequences' own workgroups fill it by themselves: 64 single tokens behind 8192 keys
     // with 4, 8, 16 and 32 of them 53, 37, 43 and 52 us; 5 x 7 behind 30011, where they do not, with 8, 16, 32 and 64 56, 34, 24.5 and 25.6.
     c.pass = rows <= 32 ? kAttentionRows : kAttentionTiles;

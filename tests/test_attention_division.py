@@ -69,3 +69,14 @@ def test_prefixes_that_leave_the_sequences_as_they_are(sizes):
 def test_prefixes_that_are_most_of_the_keys():
     assert _prefix(2, 2, 3000, 400, 8, 2, 64) == (0, 1, 3, 0)
     assert _prefix(3, 6, 2000, 900, 32, 8, 64) == (0, 1, 3, 0)
+
+
+@pytest.mark.parametrize("sizes", BATCHES[:4] + [(32, 32, 32 * 2000, 32, 8), (24, 48, 24 * 5000, 16, 8)])
+def test_own_keys_behind_many_shared_ones(sizes):
+    sequences, Tq, Tk, H, G = sizes
+    in_parts, _, own, _ = _prefix(sequences, Tq, 4096, Tk, H, G, 128)
+    assert in_parts and own == min(_attention(*sizes)[1], 5)
+
+
+def test_parts_of_many_rows_are_few():
+    assert _prefix(64, 6400, 9000, 64 * 2000, 8, 8, 128)[::2] == (1, 0)
