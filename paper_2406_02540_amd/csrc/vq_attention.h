@@ -150,6 +150,27 @@ inline long shared_blocks(long tiles, int split_shift, int kv_heads) {
     return (((long)kv_heads << split_shift) + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds * tiles;
 }
 
+// Blocks of ROWS rows of all sequences are numbered so that a sequence's first is floor(cu * group / ROWS) + b, at least the blocks of the
+// sequences in front of it (floor(x + y) - floor(x) + 1 >= ceil(y)): a sequence is found by bisection, and a number that no block has
+// is a workgroup that ends at once.
+template <int ROWS, class ARGS>
+__device__ __forceinline__ int find_sequence(const ARGS& a, int item, int& block) {
+    int lo = 0, hi = a.sequences - 1;
+    auto first = [&](int b) { return (int)((unsigned)(min(max(a.cu_q[b], 0), a.Tq) * a.group) / ROWS) + b; };
+    while (lo < hi) {
+        const int mid = lo + (hi - lo + 1) / 2;
+        if (first(mid) <= item) lo = mid;
+        else hi = mid - 1;
+    }
+    block = item - first(lo);
+    return lo;
+}
+template <int ROWS>
+__device__ __forceinline__ int find_sequence(const AttentionSharedArgs&, int item, int& block) {
+    block = item;
+    return 0;
+}
+
 // ---- which keys there are ------------------------------------------------------------------------------------
 // The keys that a block of a sequence's query rows works on, in tiles of N, for the arguments ARGS; tokens ascend along the block's rows.
 

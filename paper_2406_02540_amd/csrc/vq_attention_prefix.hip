@@ -32,7 +32,10 @@ AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix,
         return c;
     }
     c.in_parts = true;
-    const long own_items = (long)sequences * kv_heads;
+    // Where there are more than single tokens, a workgroup for every block of rows: a prompt among single tokens would take all of its own one after another.
+    // 63 single tokens and a prompt of 1900 behind 4000 keys, 32 heads on 8 of 128, 3370 us by sequences and 233, a prompt of 400 295 and 62.
+    c.by_blocks = Tq > sequences;
+    const long own_blocks = c.by_blocks ? rows / kOwnRows + sequences : sequences, own_items = own_blocks * kv_heads;
     // Own keys of few rows are divided as vq_attention's (at most 32 parts of them and 32 of the shared ones): single tokens of up to 32768 keys, 12000 on
     // average, 32 heads on 8 of 128, behind 4096 others with workgroups for two turns of the chip and for eight, 16 sequences 237 us and 182, 48 583 and 481;
     // 32 of up to 8000 behind 2048 110 and 91; 8 equal ones of 16000 behind 8192 114 and 117, 64 of 4096 220 and 224.
@@ -41,8 +44,9 @@ AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix,
     // with 4, 8, 16 and 32 of them 53, 37, 43 and 52 us; 5 x 7 behind 30011, where they do not, with 8, 16, 32 and 64 56, 34, 24.5 and 25.6.
     c.pass = rows <= 32 ? kAttentionRows : kAttentionTiles;
     const long tiles = c.pass == kAttentionRows ? 1 : (rows + kTileRows - 1) / kTileRows;
-    while (c.shared_shift < 5 && (tiles * kv_heads << c.shared_shift) < (own_items >= 256 ? 128 : 384) && (long)prefix >> (c.shared_shift + 1) >= 256) ++c.shared_shift;
-    c.fits = (groups(sequences, c.split_shift) + shared_blocks(tiles, c.shared_shift, kv_heads)) * 256 < 1l << 32;
+    while (c.shared_shift < 5 && (tiles * kv_heads << c.shared_shift) < ((long)sequences * kv_heads >= 256 ? 128 : 384) && (long)prefix >> (c.shared_shift + 1) >= 256) ++c.shared_shift;
+    c.fits = (groups(own_blocks, c.split_shift) + shared_blocks(tiles, c.shared_shift, kv_heads)) * 256 < 1l << 32;
+    c.own_items = c.fits ? (int)own_blocks : 0;
     return c;
 }
 
@@ -80,7 +84,7 @@ hipError_t launch(const AttentionPrefixArgs& a, const AttentionPrefixChoice& cho
         const hipError_t e = choice.pass == kAttentionTiles ? launch_tiles<TYPE>(a, stream) : launch_rows<TYPE, 4, 2>(a, stream);
         return e != hipSuccess || a.split_shift == 0 ? e : launch_join<AttentionArgs>(a, dtype, stream);
     }
-    PartsArgs p{{a}, {a}, 0};
+    PartsArgs p{{a}, {a, 0}, 0};
     AttentionSharedArgs& s = p.shared;
     s.k = a.prefix_k, s.v = a.prefix_v, s.Tk = a.prefix, s.causal = 0, s.split_shift = choice.shared_shift;
     s.k_token = a.pk_token, s.k_head = a.pk_head, s.v_token = a.pv_token, s.v_head = a.pv_head;
@@ -88,7 +92,8 @@ hipError_t launch(const AttentionPrefixArgs& a, const AttentionPrefixChoice& cho
     p.shared_blocks = (unsigned)shared_blocks(s.tiles, s.split_shift, a.kv_heads);
     const size_t behind = ((size_t)a.Tq << choice.shared_shift) * a.heads;
     p.own.part_o += behind * a.head_dim, p.own.part_ml += behind * 2;
-    const unsigned blocks = p.shared_blocks + attention_grid(p.own, a.sequences);
+    p.own.by_blocks = choice.by_blocks;
+    const unsigned blocks = p.shared_blocks + attention_grid(p.own, choice.own_items);
     const hipError_t e = choice.pass == kAttentionTiles ? launch_parts<TYPE, kAttentionTiles>(p, blocks, stream) : launch_parts<TYPE, kAttentionRows>(p, blocks, stream);
     if (e != hipSuccess) return e;
     AttentionPrefixArgs join = a;
@@ -110,4 +115,7 @@ extern "C" void vq_internal_attention_prefix_choice(int sequences, int Tq, int p
     choice[1] = c.pass;
     choice[2] = c.split_shift;
     choice[3] = c.shared_shift;
+}
+extern "C" int vq_internal_attention_prefix_own_items(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim) {
+    return vq::choose_attention_prefix(sequences, Tq, prefix, Tk, heads, kv_heads, head_dim).own_items;
 }

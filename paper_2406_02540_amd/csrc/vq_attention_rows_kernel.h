@@ -7,6 +7,7 @@ namespace vq {
 namespace {
 
 constexpr int kRows = 32;       // query rows of a tile: the columns of an MFMA block
+constexpr int kOwnRows = 64;    // of a workgroup of a part of the sequences' own keys, one tile behind the other
 constexpr int kRowKeys = 32;       // keys of a wavefront's tile
 
 // Eight channels of a row: normalised to the output.
@@ -39,6 +40,20 @@ constexpr int kRowsBytes = [] {       // of LDS: the stages, or where the wavefr
     return stages > sums ? stages : sums;
 }();
 
+// A workgroup's sequence and rows: all of them, or a block (its number less than 2^24; the last ones see the most keys and go first).  Blocks that no
+// sequence has cost their workgroups' start: 200 x 16 tokens behind 2000 keys, 16 heads on 8 of 128, 106 us by sequences, 108 in blocks of 64
+// rows, 121 of 32; 20 x 25 behind 6000, 32 heads, 91, 85 and 79.
+struct RowsTaken {
+    int sequence, first, count;
+};
+__device__ __forceinline__ RowsTaken rows_taken(const AttentionArgs&, int item) { return {item, 0, 0x7FFFFFFF}; }
+__device__ __forceinline__ RowsTaken rows_taken(const AttentionOwnArgs& a, int item) {
+    if (!a.by_blocks) return {item, 0, 0x7FFFFFFF};
+    int block;
+    const int b = find_sequence<kOwnRows>(a, a.tiles - 1 - item, block);
+    return {b, max(block, 0) * kOwnRows, block < 0 ? 0 : kOwnRows};
+}
+
 // Workgroup `block` of a launch's.
 template <class TYPE, int CHUNKS, int STEPS, int WAVES, int STAGES, class ARGS>
 __device__ __forceinline__ void rows_of(const ARGS& a, unsigned block, char* lds) {
@@ -53,9 +68,10 @@ __device__ __forceinline__ void rows_of(const ARGS& a, unsigned block, char* lds
     const int half = lane >> 5;
     int kv, item;
     if (!place_of(a, block, kv, item)) return;
-    const int split = item & ((1 << a.split_shift) - 1), b = item >> a.split_shift;
-    const Span s = span_of(a, b);
-    const int rows = s.n * a.group;
+    const int split = item & ((1 << a.split_shift) - 1);
+    const RowsTaken taken = rows_taken(a, item >> a.split_shift);
+    const Span s = span_of(a, taken.sequence);
+    const int rows = s.n * a.group, end = taken.count < rows - taken.first ? taken.first + taken.count : rows;
     const int head_bytes = 2 * a.head_dim;
     lds_bytes const mine_in_lds = (lds_bytes)lds + wave * STAGES * kStage;
     const unsigned base = (unsigned)(uintptr_t)mine_in_lds;
@@ -66,7 +82,7 @@ __device__ __forceinline__ void rows_of(const ARGS& a, unsigned block, char* lds
     const KeyReader<CHUNKS, STEPS> k_read(mine_in_lds, lane);
     const ValueReader<CHUNKS> v_read(mine_in_lds, lane);
 
-    for (int row0 = 0; row0 < rows; row0 += kRows) {
+    for (int row0 = taken.first; row0 < end; row0 += kRows) {
         const int r = min(row0 + (lane & 31), rows - 1);
         const bool real = row0 + (lane & 31) < rows;
         const int token = token_of(a, r), head = kv * a.group + r - token * a.group;

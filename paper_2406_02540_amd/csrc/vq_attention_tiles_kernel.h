@@ -12,26 +12,6 @@ constexpr int kTileWaves = 4;
 constexpr int kTileKeys = 64;
 constexpr float kSlack = 8.0f;    // base 2: how far a score may exceed the reference before sums and outputs are rescaled
 
-// Tiles of all sequences are numbered so that a sequence's first is floor(cu * group / rows) + b, at least the tiles of the
-// sequences in front of it (floor(x + y) - floor(x) + 1 >= ceil(y)): a sequence is found by bisection, and a number that no tile has
-// is a workgroup that ends at once.
-template <class ARGS>
-__device__ __forceinline__ int find_sequence(const ARGS& a, int item, int& tile) {
-    int lo = 0, hi = a.sequences - 1;
-    auto first = [&](int b) { return (int)((unsigned)(min(max(a.cu_q[b], 0), a.Tq) * a.group) / kTileRows) + b; };
-    while (lo < hi) {
-        const int mid = lo + (hi - lo + 1) / 2;
-        if (first(mid) <= item) lo = mid;
-        else hi = mid - 1;
-    }
-    tile = item - first(lo);
-    return lo;
-}
-__device__ __forceinline__ int find_sequence(const AttentionSharedArgs&, int item, int& tile) {
-    tile = item;
-    return 0;
-}
-
 template <int CHUNKS>
 constexpr int kTilesBytes = 4 * kTileKeys * CHUNKS * 16;      // of LDS: two tiles of K, two of V
 
@@ -49,7 +29,7 @@ __device__ __forceinline__ void tiles_of(const ARGS& a, unsigned block, char* ld
     const int split = item & ((1 << a.split_shift) - 1);
     int tile;
     // (the last tiles of a sequence see the most keys: they go first)
-    const int b = find_sequence(a, a.tiles - 1 - (item >> a.split_shift), tile);
+    const int b = find_sequence<kTileRows>(a, a.tiles - 1 - (item >> a.split_shift), tile);
     const Span s = span_of(a, b);
     const int rows = s.n * a.group;
     if (tile < 0 || (unsigned)tile * kTileRows >= (unsigned)rows) return;

@@ -194,6 +194,8 @@ struct AttentionPrefixChoice {
     AttentionKernel pass;     // of the one pass, or of the rows with the shared keys
     int split_shift;          // of the one pass, or of the sequences' own keys
     int shared_shift;         // 2^shared_shift parts of the shared keys
+    bool by_blocks;           // the rows with their own keys: a workgroup takes a block of them, otherwise a sequence's
+    int own_items;            // how many of either
     bool fits;
     int parts() const { return in_parts ? (1 << split_shift) + (1 << shared_shift) : split_shift ? 1 << split_shift : 0; }
 };
@@ -202,7 +204,9 @@ AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix,
 hipError_t launch_attention_prefix(const AttentionPrefixArgs& a, const AttentionPrefixChoice& choice, int dtype, hipStream_t stream);
 // The passes of the parts: AttentionArgs of the shared keys (as keys of one sequence), and of the sequences with their own.
 struct AttentionSharedArgs : AttentionArgs {};
-struct AttentionOwnArgs : AttentionArgs {};
+struct AttentionOwnArgs : AttentionArgs {
+    int by_blocks;            // a workgroup takes a block of a sequence's rows, otherwise all of them
+};
 
 }  // namespace vq
 
@@ -213,4 +217,5 @@ extern "C" void vq_internal_mx4_choice(int M, int N, int K, int num_cus, int cho
 extern "C" void vq_internal_attention_choice(int sequences, int Tq, int Tk, int heads, int kv_heads, int choice[2]);
 extern "C" void vq_internal_attention_window_choice(int sequences, int Tq, int Tk, int heads, int kv_heads, int causal, int left, int right, int sinks, int choice[2]);
 extern "C" void vq_internal_attention_prefix_choice(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim, int choice[4]);
+extern "C" int vq_internal_attention_prefix_own_items(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim);
 extern "C" int vq_internal_gemm_out(int N, const void* y, const void* acc_out);

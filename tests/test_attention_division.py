@@ -80,3 +80,17 @@ def test_own_keys_behind_many_shared_ones(sizes):
 
 def test_parts_of_many_rows_are_few():
     assert _prefix(64, 6400, 9000, 64 * 2000, 8, 8, 128)[::2] == (1, 0)
+
+
+def _own_items(sequences, Tq, P, Tk, H, G, D):
+    return binding.lib().vq_internal_attention_prefix_own_items(sequences, Tq, P, Tk, H, G, D)
+
+
+def test_rows_with_their_own_keys_are_no_chain():
+    # sequences of more than a token: a workgroup a head for every block of 64 rows, whatever sequence it is of
+    for sequences, tokens, H, G, D in ((64, 1963, 32, 8, 128), (16, 812, 16, 8, 64), (61, 460, 8, 2, 64), (200, 3200, 16, 8, 128)):
+        sizes = sequences, tokens, 8192, 100 * sequences, H, G, D
+        assert _prefix(*sizes)[0] == 1
+        assert _own_items(*sizes) == tokens * (H // G) // 64 + sequences
+    # single tokens: one for every sequence
+    assert _prefix(64, 64, 8192, 6400, 32, 8, 128)[0] == 1 and _own_items(64, 64, 8192, 6400, 32, 8, 128) == 64
