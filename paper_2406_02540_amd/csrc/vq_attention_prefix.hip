@@ -20,8 +20,9 @@ AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix,
     // own traffic weighs.  Parts and one pass (us; heads on heads of k and v): 8 single tokens behind 4096 keys, 32 on 8 of 128, 15 and 26; 16 behind 512
     // 13.3 and 16.3; 2 behind 8192 17.7 and 19.0; 3 x 4 behind 4096, 16 on 2 of 64 (4 MB), 12.6 and 12.1; 12 x 30 behind 3000, 16 on 8 of 64, 25 and 41, x 64 37 and
     // 47; 64 x 100 behind 4000, 8 of 128, 153 and 208; 200 x 64 behind 1000, 16 of 72, 228 and 170.
-    const long again = (long)(sequences - 1) * prefix * kv_heads * head_dim * 4, own = (long)Tk / sequences;
-    if (again < 8l << 20 || (rows > 32l * sequences && (rows > 128l * sequences || prefix < 2048 || own > prefix / 4))) {
+    const double again = 4.0 * (sequences - 1) * prefix * kv_heads * head_dim;       // (beyond 2^63 where sizes are the largest)
+    const long own = (long)Tk / sequences;
+    if (again < 8 << 20 || (rows > 32l * sequences && (rows > 128l * sequences || prefix < 2048 || own > prefix / 4))) {
         c.pass = rows > 32l * sequences ? kAttentionTiles : kAttentionRows;
         const long keys = own + prefix, tiles = c.pass == kAttentionTiles ? attention_items(sequences, Tq, group) : sequences;
         // (sequences are about equal where the prefix is most of what they have. 16 single tokens of up to 32768 keys, 12000 on average, 32 heads on 8

@@ -94,3 +94,13 @@ def test_rows_with_their_own_keys_are_no_chain():
         assert _own_items(*sizes) == tokens * (H // G) // 64 + sequences
     # single tokens: one for every sequence
     assert _prefix(64, 64, 8192, 6400, 32, 8, 128)[0] == 1 and _own_items(64, 64, 8192, 6400, 32, 8, 128) == 64
+
+
+def test_the_largest_sizes():
+    # (their products with the bytes of a key pass 63 bits; views may repeat one key)
+    most = 2**31 - 768
+    for sequences in (1 << 22, 1 << 23, (1 << 23) + 999):
+        for tokens in (sequences, 2 * sequences):
+            assert _prefix(sequences, tokens, most, 0, 1, 1, 128)[0] == 1, sequences
+    bytes_of = binding.lib().vq_attention_prefix_workspace_bytes
+    assert [bytes_of(2**31 - 1, tokens, most, 0, G, G, 128) for G in (1, 8, 1 << 16) for tokens in (1, 2**31 // G - 256)] == [0] * 6
