@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import importlib.machinery
 import importlib.util
+import operator
 import os
 import re
 
@@ -330,13 +331,19 @@ def vq_norm_rotary(q, k, q_weight=None, k_weight=None, q_bias=None, k_bias=None,
                                          sections, _named(ROPE_PAIRS, pairing, "pairing"), amplitude, q_out, k_out, stream)
 
 
-def _limit(n):
-    return -1 if n is None else int(n)
+def _int(n) -> int:
+    """n as the library's int; what does not fit is a number that it takes for nothing (ctypes would cut it to another)."""
+    n = int(n)
+    return n if -2**31 <= n < 2**31 else -2**31
+
+
+def _limit(n) -> int:
+    return -1 if n is None else _int(operator.index(n))
 
 
 def vq_attention_window_workspace_bytes(sequences, Tq, Tk, heads, kv_heads, head_dim, causal, left, right, sinks) -> int:
-    return int(lib().vq_attention_window_workspace_bytes(int(sequences), int(Tq), int(Tk), int(heads), int(kv_heads), int(head_dim),
-                                                         int(causal), _limit(left), _limit(right), int(sinks)))
+    return int(lib().vq_attention_window_workspace_bytes(_int(sequences), _int(Tq), _int(Tk), _int(heads), _int(kv_heads), _int(head_dim),
+                                                         int(bool(causal)), _limit(left), _limit(right), _int(operator.index(sinks))))
 
 
 def vq_attention_window(q, k, v, cu_q, cu_k, left, right=None, sinks=0, softmax_scale=None, causal=False, out=None, workspace=None,
@@ -347,8 +354,8 @@ def vq_attention_window(q, k, v, cu_q, cu_k, left, right=None, sinks=0, softmax_
 
 
 def vq_attention_prefix_workspace_bytes(sequences, Tq, prefix, Tk, heads, kv_heads, head_dim) -> int:
-    return int(lib().vq_attention_prefix_workspace_bytes(int(sequences), int(Tq), int(prefix), int(Tk), int(heads), int(kv_heads),
-                                                         int(head_dim)))
+    return int(lib().vq_attention_prefix_workspace_bytes(_int(sequences), _int(Tq), _int(prefix), _int(Tk), _int(heads), _int(kv_heads),
+                                                         _int(head_dim)))
 
 
 def vq_attention_prefix(q, prefix_k, prefix_v, k, v, cu_q, cu_k, softmax_scale=None, causal=False, out=None, workspace=None, stream=None):
