@@ -218,4 +218,6 @@ extern "C" void vq_internal_attention_choice(int sequences, int Tq, int Tk, int 
 extern "C" void vq_internal_attention_window_choice(int sequences, int Tq, int Tk, int heads, int kv_heads, int causal, int left, int right, int sinks, int choice[2]);
 extern "C" void vq_internal_attention_prefix_choice(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim, int choice[4]);
 extern "C" int vq_internal_attention_prefix_own_items(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim);
+extern "C" void vq_internal_rotary_axes_choice(int norm, int has_bias, int pairing, int axes, const int32_t* sections, int T, int q_heads, int k_heads, int head_dim,
+                                               const int64_t* strides, int choice[4]);
 extern "C" int vq_internal_gemm_out(int N, const void* y, const void* acc_out);

@@ -292,9 +292,13 @@ void (*kernel_of(int grain, bool wide))(RotaryAxesArgs) {
     return wide ? kernel_of<TYPE, NORM, true>(grain) : kernel_of<TYPE, NORM, false>(grain);
 }
 
-}  // namespace
-
-hipError_t launch_rotary_axes(RotaryAxesArgs a, int dtype, hipStream_t stream) {
+// Fills in what a workgroup takes, and says which kernel takes it.
+struct Choice {
+    int grain;
+    bool wide;
+    size_t lds;
+};
+Choice choose(RotaryAxesArgs& a) {
     // Channels that keep together on their way to their partners: 8, or the largest power of two that divides every axis' pairs, or all
     // pairs where they are halves of the whole.
     int all = a.pairing == VQ_PAIRS_HALVES ? a.pairs : 0;
@@ -331,14 +335,37 @@ hipError_t launch_rotary_axes(RotaryAxesArgs a, int dtype, hipStream_t stream) {
     auto extent = [&](int64_t token, int64_t head, int heads) { return 2 * ((a.tokens_each - 1) * token + (heads - 1) * head + a.head_dim); };
     bool wide = extent(a.q_token, a.q_head, a.q_heads) >= 1l << 31 || extent(a.qo_token, a.qo_head, a.q_heads) >= 1l << 31;
     if (a.k_heads) wide = wide || extent(a.k_token, a.k_head, a.k_heads) >= 1l << 31 || extent(a.ko_token, a.ko_head, a.k_heads) >= 1l << 31;
+    return {grain, wide, lds_of(a.tokens_each)};
+}
+
+}  // namespace
+
+hipError_t launch_rotary_axes(RotaryAxesArgs a, int dtype, hipStream_t stream) {
+    const Choice c = choose(a);
     void (*kernel)(RotaryAxesArgs) = nullptr;
     const bool f16 = dtype == VQ_F16;
     switch (a.norm) {
-        case 0: kernel = f16 ? kernel_of<F16, 0>(grain, wide) : kernel_of<BF16, 0>(grain, wide); break;
-        case 1 + VQ_NORM_RMS: kernel = f16 ? kernel_of<F16, 1 + VQ_NORM_RMS>(grain, wide) : kernel_of<BF16, 1 + VQ_NORM_RMS>(grain, wide); break;
-        default: kernel = f16 ? kernel_of<F16, 1 + VQ_NORM_LAYER>(grain, wide) : kernel_of<BF16, 1 + VQ_NORM_LAYER>(grain, wide); break;
+        case 0: kernel = f16 ? kernel_of<F16, 0>(c.grain, c.wide) : kernel_of<BF16, 0>(c.grain, c.wide); break;
+        case 1 + VQ_NORM_RMS: kernel = f16 ? kernel_of<F16, 1 + VQ_NORM_RMS>(c.grain, c.wide) : kernel_of<BF16, 1 + VQ_NORM_RMS>(c.grain, c.wide); break;
+        default: kernel = f16 ? kernel_of<F16, 1 + VQ_NORM_LAYER>(c.grain, c.wide) : kernel_of<BF16, 1 + VQ_NORM_LAYER>(c.grain, c.wide); break;
     }
-    return enqueue(kernel, dim3((unsigned)(a.blocks < 1 << 20 ? a.blocks : 1 << 20)), dim3(64 * kWaves), stream, a, lds_of(a.tokens_each));
+    return enqueue(kernel, dim3((unsigned)(a.blocks < 1 << 20 ? a.blocks : 1 << 20)), dim3(64 * kWaves), stream, a, c.lds);
 }
 
 }  // namespace vq
+
+extern "C" void vq_internal_rotary_axes_choice(int norm, int has_bias, int pairing, int axes, const int32_t* sections, int T, int q_heads, int k_heads, int head_dim,
+                                               const int64_t* strides, int choice[4]) {
+    const float bias = 0;
+    vq::RotaryAxesArgs a{};
+    a.norm = norm, a.bias[0] = has_bias ? &bias : nullptr, a.pairing = pairing, a.axes = axes;
+    for (int i = 0; i < axes; ++i) a.sections[i] = sections[i], a.pairs += sections[i];
+    a.T = T, a.q_heads = q_heads, a.k_heads = k_heads, a.head_dim = head_dim;
+    a.q_token = strides[0], a.q_head = strides[1], a.qo_token = strides[2], a.qo_head = strides[3];
+    a.k_token = strides[4], a.k_head = strides[5], a.ko_token = strides[6], a.ko_head = strides[7];
+    const vq::Choice c = vq::choose(a);
+    choice[0] = c.grain;
+    choice[1] = c.wide;
+    choice[2] = a.tokens_each;
+    choice[3] = a.heads_each;
+}
