@@ -352,7 +352,7 @@ size_t vq_linear_mx4_workspace_bytes(int M, int N, int K);
  *       out_a = a c - b s,   out_b = b c + a s,
  *   with (a, b) = channels (i, i + rot_dim/2), or (2i, 2i+1) if interleaved.  The angle is
  *   reduced in 64 bits (positions far into a long context keep it), products and sums are fp32.
- *   Channels from rot_dim on are copied.
+ *   Channels from rot_dim on are copied.  (vq_rotary_axes with one axis does the same, faster where a part of heads of 72 channels is turned.)
  *     q, q_out   [T, q_heads, head_dim]; k, k_out likewise with k_heads (k_heads = 0: none)
  *     positions  int32 [T], any value (the negative of a position undoes it)
  *     inv_freq   fp32 [rot_dim/2]
@@ -416,6 +416,8 @@ size_t vq_attention_workspace_bytes(int sequences, int Tq, int Tk, int heads, in
  *   rot_dim = 2 (sections[0] + ... ), at most head_dim; channels from rot_dim on are copied.
  *     positions  int32 [axes, T], any values
  *     inv_freq   fp32 [rot_dim/2] (vq_rotary_frequencies of 2 * sections[a] channels for every axis, one behind the other)
+ *   One axis is vq_rotary's rotation, its fp32 operations rounded in another order.  Which of the two: this one for many tokens in halves, and where
+ *   heads are no whole lines of 128 bytes and a part of them is turned (36 of 72 channels: half the time); vq_rotary for a few tokens.
  *     sections   host, axes of them, each at least 1; axes 1 to VQ_MAX_AXES
  *
  * vq_norm_rotary: the norm of every head of q and k, and the rotation behind it in the same pass.

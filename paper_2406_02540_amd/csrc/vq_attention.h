@@ -86,8 +86,8 @@ __device__ __forceinline__ bool place_of(const AttentionArgs& a, unsigned block,
     return item < a.items;
 }
 // With a window and heads of no whole lines, runs of items go to one XCD with eight neighbouring heads, whose rows share memory lines of all
-// tensors; the items of a run, neighbouring blocks of rows, share most of their keys too.  2 x 16384 tokens, 16 heads of 72, windows of 2049: 486 us by
-// heads, 472 in runs of one, 457 of eight; of 257: 139, 127 and 125; of 1024, causal: 285, 268, 260.  Heads of 64 are better by heads, 364 and 381.
+// tensors; the items of a run, neighbouring blocks of rows, share most of their keys too.  2 x 16384 tokens, 16 heads of 72, windows of 2049: 468 us by
+// heads, 453 in runs of one, 440 of eight; of 257: 119, 120 and 117; of 1024, causal: 274, 257, 248.  Heads of 64 are better by heads, 362 and 376.
 constexpr int kHeadsOfRun = 8;
 __device__ __forceinline__ bool place_of(const AttentionWindowArgs& a, unsigned block, int& kv, int& item) {
     if (a.run == 0) return place_of(static_cast<const AttentionArgs&>(a), block, kv, item);

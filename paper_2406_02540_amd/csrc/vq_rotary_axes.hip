@@ -4,7 +4,7 @@
 //     out_c = r ((x_c - mean) w_c A_c + (x_p - mean) w_p B_c) + (b_c A_c + b_p B_c):
 // what depends on token and channel alone is a table in LDS, made once for all heads of a workgroup's tokens, and a head costs two
 // products a channel, whatever the order of its pairs.  All of it fp32, one rounding at the end.  Reads and writes every value once: bound by
-// memory (a copy of 1 GiB moves 5.1 TB/s).
+// memory (a copy of 1 GiB moves 5.1 TB/s; outputs that the last-level cache holds from the call before go faster).
 #include <type_traits>
 
 #include "vq_internal.h"
@@ -118,8 +118,9 @@ struct Side {
 // a token's heads lie next to each other.  Partners are read where the wavefront's rows pass through LDS, GRAIN channels at once: as many as
 // every axis' pairs divide by (0: neighbours, which a lane has itself).  NORM: 0, or 1 + vq_norm.  WIDE: a workgroup's rows are more than 2^31
 // bytes apart.  kAtOnce rows of a lane are worked on together, the next ones' loads on their way meanwhile; six workgroups a CU cover each
-// other's waits.  32768 tokens, 16 + 16 heads of 72, f16: turned 50 us (6.0 TB/s), normed and turned 55 us (5.5), with mean, variance and biases 65; with four rows
-// at once, four workgroups a CU, 58, 67 and 82; one row, seven a CU, 52, 59 and 70 (inputs that are not in the caches).
+// other's waits.  32768 tokens, 16 + 16 heads of 72, f16, with outputs of their own, turned 61 us (5.0 TB/s), normed and turned 62.  Launches whose outputs
+// go where the last one's went, inputs that are not in the caches: 50, 55 and with mean, variance and biases 65; with four rows at once, four workgroups a CU,
+// 58, 67 and 82; one row, seven a CU, 52, 59 and 70.
 template <class TYPE, int GRAIN, int NORM, bool WIDE>
 __global__ __launch_bounds__(64 * kWaves, WIDE || GRAIN == 1 ? 5 : 6) void rotary_axes(RotaryAxesArgs a) {
     typedef typename std::conditional<WIDE, int64_t, unsigned>::type Offset;
