@@ -14,7 +14,6 @@ namespace vq {
 AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix, int Tk, int heads, int kv_heads, int head_dim) {
     const int group = heads / kv_heads;
     const long rows = (long)Tq * group;          // of all sequences
-    AttentionPrefixChoice c{};
     auto groups = [&](long tiles, int shift) { return ((tiles << shift) + kAttentionXcds - 1) / kAttentionXcds * kAttentionXcds * kv_heads; };
     // In parts where one pass would read at least 8 MB of shared keys over and over, and a sequence's rows leave tiles of 128 as empty as the parts'
     // own traffic weighs.  Parts and one pass (us; heads on heads of k and v): 8 single tokens behind 4096 keys, 32 on 8 of 128, 15 and 26; 16 behind 512
@@ -22,7 +21,8 @@ AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix,
     // 47; 64 x 100 behind 4000, 8 of 128, 153 and 208; 200 x 64 behind 1000, 16 of 72, 228 and 170.
     const double again = 4.0 * (sequences - 1) * prefix * kv_heads * head_dim;       // (beyond 2^63 where sizes are the largest)
     const long own = (long)Tk / sequences;
-    if (again < 8 << 20 || (rows > 32l * sequences && (rows > 128l * sequences || prefix < 2048 || own > prefix / 4))) {
+    auto one_pass = [&] {
+        AttentionPrefixChoice c{};
         c.pass = rows > 32l * sequences ? kAttentionTiles : kAttentionRows;
         const long keys = own + prefix, tiles = c.pass == kAttentionTiles ? attention_items(sequences, Tq, group) : sequences;
         // (sequences are about equal where the prefix is most of what they have. 16 single tokens of up to 32768 keys, 12000 on average, 32 heads on 8
@@ -31,7 +31,9 @@ AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix,
                                                                   : split_for(c.pass == kAttentionRows ? kRaggedWorkgroups : 512, tiles * kv_heads, keys);
         c.fits = groups(tiles, c.split_shift) * 256 < 1l << 32;
         return c;
-    }
+    };
+    if (again < 8 << 20 || (rows > 32l * sequences && (rows > 128l * sequences || prefix < 2048 || own > prefix / 4))) return one_pass();
+    AttentionPrefixChoice c{};
     c.in_parts = true;
     // Where there are more than single tokens, a workgroup for every block of rows: a prompt among single tokens would take all of its own one after another.
     // 63 single tokens and a prompt of 1900 behind 4000 keys, 32 heads on 8 of 128, 3370 us by sequences and 233, a prompt of 400 295 and 62.
@@ -46,8 +48,10 @@ AttentionPrefixChoice choose_attention_prefix(int sequences, int Tq, int prefix,
     c.pass = rows <= 32 ? kAttentionRows : kAttentionTiles;
     const long tiles = c.pass == kAttentionRows ? 1 : (rows + kTileRows - 1) / kTileRows;
     while (c.shared_shift < 5 && (tiles * kv_heads << c.shared_shift) < ((long)sequences * kv_heads >= 256 ? 128 : 384) && (long)prefix >> (c.shared_shift + 1) >= 256) ++c.shared_shift;
-    c.fits = (groups(own_blocks, c.split_shift) + shared_blocks(tiles, c.shared_shift, kv_heads)) * 256 < 1l << 32;
-    c.own_items = c.fits ? (int)own_blocks : 0;
+    // (parts take more workgroups than one pass: where a launch does not hold them it is one pass)
+    if ((groups(own_blocks, c.split_shift) + shared_blocks(tiles, c.shared_shift, kv_heads)) * 256 >= 1l << 32) return one_pass();
+    c.fits = true;
+    c.own_items = (int)own_blocks;
     return c;
 }
 
