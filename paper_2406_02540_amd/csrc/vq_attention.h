@@ -133,7 +133,8 @@ constexpr int kItemsRounded = 8 * kAttentionXcds;      // a launch's items are r
 // 31.5 and 38.5, 1000 51 and 53.
 inline int split_of_equal(long items, long keys) {
     int best = 0;
-    for (int shift = 1; shift <= 6 && keys >> shift >= 256; ++shift) {
+    // (up to 2^16 items, 256 turns: of more the last turn is next to nothing, and a launch has to hold them)
+    for (int shift = 1; shift <= 6 && keys >> shift >= 256 && items << shift <= 1 << 16; ++shift) {
         auto cost = [&](int s) { return (((items << s) + 255) / 256) * ((keys >> s) + 256) + (s ? 256 : 0); };
         if (cost(shift) < cost(best)) best = shift;
     }

@@ -2,6 +2,7 @@
 gets as far as the device's check was accepted."""
 import ctypes
 import os
+import random
 
 import pytest
 
@@ -34,6 +35,20 @@ def _check(lib, B, Tq, P_, Tk, H, G, D):
     for name, rounded, call in _calls(lib, B, Tq, P_, Tk, H, G, D):
         if Tq * H / 128 + (B + rounded) * G < 2**24:
             assert call() == ARCH, (name, B, Tq, P_, Tk, H, G, D)
+
+
+def test_random_sizes(lib):
+    r = random.Random(7)
+    for _ in range(20000):
+        G = r.choice((1, 1, 2, 3, 7, 8, 64))
+        H = G * r.choice((1, 2, 4, 7, 48))
+        Tq = int(2 ** r.uniform(0, 31)) % (MOST // H) + 1
+        B = int(2 ** r.uniform(0, 24)) // G + 1
+        if r.random() < 0.5:                      # from single tokens to 200 rows a sequence
+            B = max(1, int(Tq / (2 ** r.uniform(0, 7.6) * G / H + 1)))
+        prefix = int(2 ** r.uniform(0, 30))
+        Tk = min(int(2 ** r.uniform(0, 31)), MOST - prefix)
+        _check(lib, B, Tq, prefix, Tk, H, G, r.choice((8, 64, 72, 128)))
 
 
 def test_many_rows_in_parts(lib):
